@@ -245,6 +245,123 @@ int32_t kvp_eval_configs_ex(const kvp_view* q_win, const kvp_view* k, const kvp_
                             int32_t n_cfgs, float* loss, float* partial, void* ws, size_t ws_bytes, uint32_t flags,
                             void* stream);
 
+/* ---- an 8-bit paged cache that is attended in place -------------------------------------------------------------
+ *
+ * The calls above store a context compressed and restore it to bf16 before it is used.  The calls below keep one
+ * layer's cache of a batch of sequences in 8 bits in the serving engine's pages, grow it, attend over it without
+ * restoring it, and shorten it by what its tokens have drawn (Background: quantization methods lower the bit width of KV
+ * entries and pay a decompression step; token dropping keeps the tokens that attention weighs most; Limitations: the
+ * method pool that joins the two).
+ *
+ * Every page holds bs tokens of all heads and has ONE scale per head for its keys and one for its values; the value of a
+ * code is code * scale.  Keys are token-major, values channel-major, so that a matrix-core operand of either is a run of
+ * consecutive bytes.  int8 codes are two's complement in [-127, 127]; e4m3 codes are the 8-bit floating-point format with
+ * 4 exponent and 3 mantissa bits, no infinity, largest magnitude 448.
+ * Token t of sequence b lies in page block_table[b * table_stride + t / bs], slot t % bs.  Slots at or behind lens[b]
+ * may hold any bytes: no call reads a meaning into them.  Entries of lens are clamped into [0, max_blocks * bs] and
+ * table entries into [0, num_blocks) when they are read, so no content of device memory can make a call fault.
+ * Limits of every call that takes a cache: D = 128; bs 16, 32, 64 or 128; B * H, num_blocks * H and
+ * max_blocks * bs below 2^31; B * H * max_blocks below 2^31; otherwise KVP_ERR_UNSUPPORTED / KVP_ERR_SHAPE. */
+enum { KVP_CACHE_INT8 = 0, KVP_CACHE_E4M3 = 1 };
+typedef struct {
+  uint8_t* k_codes;           /* device [num_blocks][H][bs][D] */
+  uint8_t* v_codes;           /* device [num_blocks][H][D][bs] */
+  float* k_scales;            /* device [num_blocks][H] */
+  float* v_scales;            /* device [num_blocks][H] */
+  const int32_t* block_table; /* device [B][max_blocks], rows table_stride entries apart */
+  const int32_t* lens;        /* device [B]: tokens in the cache (see each call for when) */
+  int64_t B, num_blocks, bs, H, D, max_blocks, table_stride;
+  int32_t format;             /* KVP_CACHE_INT8 or KVP_CACHE_E4M3 */
+} kvp_cache;
+
+/* New tokens enter the cache: rows k[b][w], v[b][w] (bf16 views [B][W][H][D]) of w < counts[b] become tokens
+ * lens[b] + w; lens holds the lengths BEFORE the call and is left as it is (it serves all layers; the caller adds
+ * counts to it afterwards).  counts is device int32 [B], entries clamped into [0, W], or NULL: W for every sequence.
+ * Rows w >= counts[b] are not read; tokens that would lie behind max_blocks * bs are dropped.  For every page, head and
+ * plane that gets tokens, with a = max|x| over the new ones and qmax = 127 (int8) or 448 (e4m3):
+ *     scale = fl32(a / qmax)                          if the page held no token,
+ *     scale = max(scale before, fl32(a / qmax))       otherwise;
+ *     where that raised the scale, the codes before become rnd(fl32(fl32(code * scale before) / scale)),
+ *     new codes are rnd(fl32(x / scale)), 0 when scale is 0 (IEEE binary32 quotients, rounded half to even to whole
+ *     numbers or to e4m3; the sign of a zero code is not specified).
+ * Slots behind the last token keep their bytes.  Pages that get tokens must belong to one sequence only (pages shared
+ * between sequences may be full ones).  Graph capture: nothing but kernels is enqueued. */
+int32_t kvp_cache_append(const kvp_cache* cache, const kvp_view* k, const kvp_view* v, const int32_t* counts, void* stream);
+
+/* Restore to bf16: out row i of sequence b is token first[b] + i, bf16_rne(fl32(code * scale)), for
+ * first[b] + i < lens[b]; other rows are left as they were.  first is device int32 [B] (entries below 0 count as 0) or
+ * NULL: 0.  k_out and v_out are bf16 views [B][R][H][D] with the same R, either may be NULL. */
+int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, const kvp_view* k_out, const kvp_view* v_out, void* stream);
+
+/* Attention over the cache: with n = lens[b] (tokens in the cache, the query tokens' own included) and
+ * m = q_lens[b], query token w < m of sequence b stands at position p = n - m + w and sees the tokens t < n, with
+ * `causal` those of t <= p.  Query heads j*G .. j*G+G-1 (G = Hq / H) read head j:
+ *     out[b][w][i] = sum over seen t of softmax_t(scale * q . k_t) v_t      (k_t, v_t: code * scale, not rounded)
+ * A row that sees no token is zero.  Rows w >= m are not written.  q_lens: device int32 [B], entries clamped into
+ * [0, W], or NULL: W.  W = 1 is a decode step.
+ * With acc_out, the weight that every token drew, summed over the G heads and the query tokens, is added to a running sum:
+ *     acc_out[b][j][t] = (acc_in ? acc_in[b][j][t] : 0) + sum over w, i of the probabilities,   t < n
+ * (device fp32, rows acc_stride floats apart, sequence b and head j at row b * H + j; acc_in may be acc_out; entries
+ * t >= n are left as they were; always the same bits for the same input).
+ * max_len: an upper bound of lens that the host knows, 0 for max_blocks * bs; it fixes how the work is shared out and the
+ * workspace, and a longer sequence is treated as if it had max_len tokens.  acc_stride >= max_len.
+ * Arithmetic: queries are split exactly into a power of two per row and 16-bit values (what lies 2^-24 below the row's
+ * largest element is rounded away), codes are exact in 16 bits, the products of both contractions run on the matrix cores
+ * with fp32 accumulation, logits, statistics and sums are fp32, probabilities are rounded to fp16 for the product
+ * with V (2^-11 relative, half of it below 2^-14 of the row's largest).  Finite q and cache contents, finite scale.
+ * Limits: those of a cache; W * G below 2^24; grid and workspace sizes below 2^31 blocks. */
+int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,
+                         const kvp_view* out, const float* acc_in, float* acc_out, int64_t acc_stride, int64_t max_len,
+                         void* ws, size_t ws_bytes, void* stream);
+/* weights: whether acc_out is given; T: max_len */
+size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t Hq, int64_t W, int64_t T, int32_t weights);
+
+/* Eviction by accumulated attention weight: of the n = min(lens[b], max_len) tokens of every (sequence, head), the
+ * m = min(n, budget) to keep are the first `sink`, the last `recent`, and of the others those with the largest
+ * acc[b][h][t], equal weights toward the lowest index.  They move, in their old order, to slots 0 .. m-1 of the pages that
+ * dst names: values fl32(code * scale) of a page's new tokens are coded again on that page's own scale, as
+ * kvp_cache_append codes them into an empty page.  keep_idx (device int32 [B][H][budget], may be NULL) receives the old
+ * indices, -1 behind m; acc_out (device fp32, rows acc_out_stride >= budget apart, may be NULL) the kept weights, entries
+ * behind m are left as they were; lens_out (device int32 [B], may be NULL) m.  dst->lens is not read and may be lens_out; lens_out must not be
+ * src->lens, acc_out must not overlap acc, and the pages that dst names must not be among those of src (both may lie in one pool).
+ * acc: device fp32, rows acc_stride >= max_len apart; NaN is out of contract.  sink + recent <= budget (KVP_ERR_SHAPE);
+ * dst->max_blocks * bs >= budget.  max_len as in kvp_cache_attend.  src and dst agree in B, H, bs and format. */
+int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64_t acc_stride, int64_t budget, int64_t sink, int64_t recent,
+                        const kvp_cache* dst, int32_t* keep_idx, float* acc_out, int64_t acc_out_stride, int32_t* lens_out,
+                        int64_t max_len, void* ws, size_t ws_bytes, void* stream);
+size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t T, int64_t budget);
+
+/* Rotary positions of queries or keys: the pairs of the first rotary_dim channels of every row of x turn by
+ * position * freq[i], i < rotary_dim / 2 (freq: device double, radians per position), and are stretched by mscale:
+ *     y_a = m (x_a cos - x_b sin),  y_b = m (x_b cos + x_a sin)
+ * KVP_ROTARY_HALF pairs channel i with i + rotary_dim / 2, KVP_ROTARY_INTERLEAVED 2i with 2i + 1; the other channels are
+ * copied.  `inverse` turns the other way: with the same mscale that is the backward of the call, with 1 / mscale its inverse.
+ * positions: device int32 (any sign), the entry of row (l, t, h) at l * pos_stride_l + t * pos_stride_t +
+ * h * pos_stride_h; a stride may be 0.  A keep list [L][H][k] (strides H*k, 1, k) gives every kept token of every
+ * head its own; keys that were rotated at one position move to another by the difference.  The angle is formed and reduced in
+ * double, sine and cosine and the rotation in fp32, the result rounded once to bf16.  out has the shape of x; it may be the same
+ * view (in place), or must not overlap it.  rotary_dim even, 2 .. 128; L <= 65535, T and T * H below 2^31. */
+enum { KVP_ROTARY_HALF = 0, KVP_ROTARY_INTERLEAVED = 1 };
+int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int32_t* positions, int64_t pos_stride_l,
+                   int64_t pos_stride_t, int64_t pos_stride_h, const double* freq, int32_t rotary_dim, int32_t layout,
+                   int32_t inverse, float mscale, void* stream);
+
+/* Host helper: freq[i] for i < rotary_dim / 2 and the matching mscale (host pointers; either output may be NULL), with
+ * f_i = base^(-2i / rotary_dim) and, for contexts `factor` (>= 1) times as long as the `original` one:
+ *     KVP_ROTARY_PLAIN   f_i
+ *     KVP_ROTARY_LINEAR  f_i / factor                     (positions pressed together)
+ *     KVP_ROTARY_NTK     the same with base * factor^(rotary_dim / (rotary_dim - 2)): the slowest pair as LINEAR, the fastest as
+ *                        it was (rotary_dim > 2)
+ *     KVP_ROTARY_YARN    with r = original * f_i / (2 pi) turns over the original context: f_i for the pairs up to the index at which r
+ *                        is `high`, f_i / factor from the one at which it is `low`, a ramp linear in i between (the two
+ *                        indices rounded outward to whole ones); mscale = 0.1 ln(factor) + 1
+ *     KVP_ROTARY_BANDED  f_i for r >= high, f_i / factor for r <= low, and (1 - u) f_i / factor + u f_i with
+ *                        u = (r - low) / (high - low) between
+ * mscale is 1 except for YARN.  0 < low < high where they are used. */
+enum { KVP_ROTARY_PLAIN = 0, KVP_ROTARY_LINEAR = 1, KVP_ROTARY_NTK = 2, KVP_ROTARY_YARN = 3, KVP_ROTARY_BANDED = 4 };
+int32_t kvp_rotary_frequencies(double base, int32_t rotary_dim, int32_t scaling, double factor, double original, double low,
+                               double high, double* freq, float* mscale);
+
 /* One sizing call for every entry point that takes (ws, ws_bytes): the bytes the call needs for the
  * sizes in `dims` (fields an operation does not use are ignored), 0 if it needs none or the sizes
  * are invalid.  The kvp_*_workspace_bytes helpers above return the same numbers. */
@@ -252,13 +369,15 @@ enum {
   KVP_WS_SCORE_TOKENS = 0, /* L, Hkv, Hq, W, T */
   KVP_WS_SCORE_KEYS = 1,   /* L, Hkv (= H), T, method */
   KVP_WS_SELECT_TOPK = 2,  /* n_rows, T, k */
-  KVP_WS_EVAL_CONFIGS = 3  /* L, Hkv, Hq, W, T, n_cfgs */
+  KVP_WS_EVAL_CONFIGS = 3, /* L, Hkv, Hq, W, T, n_cfgs */
+  KVP_WS_CACHE_ATTEND = 4, /* L (= B), Hkv (= H), Hq, W, T (= max_len), method (= weights) */
+  KVP_WS_CACHE_EVICT = 5   /* L (= B), Hkv (= H), T (= max_len), k (= budget) */
 };
 typedef struct {
   int64_t L, Hkv, Hq, W, T; /* layers, kv heads, query heads, window rows, tokens */
-  int64_t n_rows, k;        /* kvp_select_topk */
+  int64_t n_rows, k;        /* kvp_select_topk; k also kvp_cache_evict */
   int32_t n_cfgs;           /* kvp_eval_configs */
-  int32_t method;           /* kvp_score_keys */
+  int32_t method;           /* kvp_score_keys; kvp_cache_attend: whether weights are asked for */
 } kvp_dims;
 size_t kvp_workspace_bytes(int32_t op, const kvp_dims* dims);
 
@@ -321,7 +440,7 @@ const char* kvp_strerror(int32_t code);
 /* 0x00MMmmpp.  1.3: kvp_qplane carries mins and group_axis; scatter restore, score smoothing and
  * kvp_eval_configs_ex exist.  1.4: kvp_select_topk uses its workspace for long rows; kvp_dims,
  * kvp_workspace_bytes and kvp_score_tokens_static exist.  1.5: KVP_EVAL_PV_FP32, tier -1 in kvp_policy_op,
- * kvp_selftest_reciprocal. */
+ * kvp_selftest_reciprocal.  1.6: the 8-bit paged cache (kvp_cache, append, read, attend, evict) and rotary positions. */
 uint32_t kvp_version(void);
 
 #ifdef __cplusplus

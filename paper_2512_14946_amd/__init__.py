@@ -14,4 +14,8 @@ from .kvp import (  # noqa: F401
     kvp_score_workspace_bytes, kvp_select_topk, kvp_select_workspace_bytes, kvp_smooth_scores, kvp_strerror,
     kvp_version, kvp_workspace_bytes, KVP_WS_SCORE_TOKENS, KVP_WS_SCORE_KEYS, KVP_WS_SELECT_TOPK, KVP_WS_EVAL_CONFIGS,
     library_path,
+    KVCache, alloc_cache, kvp_cache_append, kvp_cache_attend, kvp_cache_attend_workspace_bytes, kvp_cache_evict,
+    kvp_cache_evict_workspace_bytes, kvp_cache_read, kvp_rotary, kvp_rotary_frequencies, KVP_CACHE_E4M3, KVP_CACHE_INT8,
+    KVP_ROTARY_BANDED, KVP_ROTARY_HALF, KVP_ROTARY_INTERLEAVED, KVP_ROTARY_LINEAR, KVP_ROTARY_NTK, KVP_ROTARY_PLAIN,
+    KVP_ROTARY_YARN, KVP_WS_CACHE_ATTEND, KVP_WS_CACHE_EVICT,
 )

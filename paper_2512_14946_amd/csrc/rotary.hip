@@ -1,0 +1,232 @@
+// kvp_rotary: rotary positions.  Every pair (a, b) of a row turns by t = position * freq[i]:
+//   y_a = m (a cos t - b sin t),  y_b = m (b cos t + a sin t)
+// The angle of a far position has too many bits for fp32 (131072 radians leave an error of 0.004), so position * freq / 2 pi and its
+// fraction are formed in double; the fraction of a turn in [-1/2, 1/2] loses nothing that matters in fp32.
+//
+// Bound by HBM (x is read and written once) except where every head has positions of its own.  A block takes some
+// tokens with all their heads; one sine and cosine per (token, pair) go to LDS once and serve every head.  Lanes then
+// stream the rows: eight lanes share a row, each owns two 16-byte pieces, which hold both channels of its eight pairs
+// (half layout: pieces rotary_dim / 2 apart).  Pairs that do not fall on such pieces (half layout, rotary_dim not a multiple
+// of 16) take a kernel with two lanes' channels per element access.
+
+#include <math.h>
+
+#include "kvp_common.h"
+
+namespace kvp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTokens = 64;                 // tokens (or rows, with a position per head) of a block
+
+struct RotaryArgs {
+  const uint16_t* x;
+  uint16_t* out;
+  int64_t x_sl, x_st, x_sh, o_sl, o_st, o_sh;  // elements
+  const int32_t* pos;
+  int64_t p_sl, p_st, p_sh;
+  const double* freq;
+  uint32_t T, H, pairs;                        // pairs = rotary_dim / 2
+  uint32_t units, unit_heads, units_block;     // a unit: the heads that share a position (unit_heads = H, or 1); units per layer, per block
+  FastDiv div_h, div_pairs;
+  float mscale, sign;
+  bool copy;                                   // out is not x: channels behind rotary_dim are copied
+};
+
+// cosine and sine (times mscale, the sine with the direction's sign) of a position's pair
+__device__ __forceinline__ float2 turn_of(const RotaryArgs& a, int32_t pos, double freq) {
+  constexpr double kTurn = 0.15915494309189535;   // 1 / (2 pi)
+  double r = static_cast<double>(pos) * freq * kTurn;
+  r -= __builtin_rint(r);
+  float s, c;
+  sincospif(2.0f * static_cast<float>(r), &s, &c);
+  return make_float2(c * a.mscale, s * a.mscale * a.sign);
+}
+
+__device__ __forceinline__ void rotate(float& x, float& y, float2 cs) {
+  const float p = fmaf(x, cs.x, -(y * cs.y)), q = fmaf(y, cs.x, x * cs.y);
+  x = p;
+  y = q;
+}
+
+__device__ __forceinline__ uint4 rotate_pair8(uint4& lo, uint4 hi, const float2* cs) {   // half layout: 8 pairs over two pieces
+  uint32_t* l = reinterpret_cast<uint32_t*>(&lo);
+  uint32_t* h = reinterpret_cast<uint32_t*>(&hi);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a0 = bf16lo(l[i]), a1 = bf16hi(l[i]), b0 = bf16lo(h[i]), b1 = bf16hi(h[i]);
+    rotate(a0, b0, cs[2 * i]);
+    rotate(a1, b1, cs[2 * i + 1]);
+    l[i] = pack_bf16x2(a0, a1);
+    h[i] = pack_bf16x2(b0, b1);
+  }
+  return hi;
+}
+
+__device__ __forceinline__ uint4 rotate_piece(uint4 v, const float2* cs, uint32_t first, uint32_t pairs) {   // interleaved: 4 pairs of a piece
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    if (first + i < pairs) {
+      float a = bf16lo(w[i]), b = bf16hi(w[i]);
+      rotate(a, b, cs[first + i]);
+      w[i] = pack_bf16x2(a, b);
+    }
+  }
+  return v;
+}
+
+// LAYOUT half: rotary_dim is a multiple of 16
+template <int LAYOUT>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
+  __shared__ float2 cs_s[kMaxTokens * 64];
+  const uint32_t l = blockIdx.y, unit0 = blockIdx.x * a.units_block, n_units = min(a.units_block, a.units - unit0);
+  const bool per_head = a.unit_heads == 1;     // a unit is a (token, head) row then
+  for (uint32_t i = threadIdx.x; i < n_units * a.pairs; i += kThreads) {
+    const uint32_t u = a.div_pairs.quot(i), p = i - u * a.pairs, unit = unit0 + u;
+    const uint32_t t = per_head ? a.div_h.quot(unit) : unit, h = per_head ? unit - t * a.H : 0;
+    const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
+    cs_s[u * 64 + p] = turn_of(a, pos, a.freq[p]);
+  }
+  __syncthreads();
+  const uint32_t rows = n_units * a.unit_heads, row0 = unit0 * a.unit_heads;
+  const uint16_t* x_l = a.x + static_cast<int64_t>(l) * a.x_sl;
+  uint16_t* o_l = a.out + static_cast<int64_t>(l) * a.o_sl;
+  const uint32_t j = threadIdx.x & 7;
+  // pieces of this lane: half layout 8 j and 8 j + rotary_dim / 2 while j < rotary_dim / 16, then two of the rest
+  uint32_t c0, c1;
+  bool turns;
+  if (LAYOUT == KVP_ROTARY_HALF) {
+    turns = 8 * j < a.pairs;
+    c0 = turns ? 8 * j : 2 * a.pairs + 16 * (j - a.pairs / 8);
+    c1 = turns ? c0 + a.pairs : c0 + 8;
+  } else {
+    turns = true;
+    c0 = 8 * j;
+    c1 = 64 + 8 * j;
+  }
+  if (!turns && !a.copy) return;
+  for (uint32_t r = threadIdx.x >> 3; r < rows; r += kThreads / 8) {
+    const uint32_t row = row0 + r, t = a.div_h.quot(row), h = row - t * a.H;
+    const uint32_t u = per_head ? r : t - unit0;
+    const uint16_t* src = x_l + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
+    uint16_t* dst = o_l + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
+    uint4 v0 = *reinterpret_cast<const uint4*>(src + c0), v1 = *reinterpret_cast<const uint4*>(src + c1);
+    if (LAYOUT == KVP_ROTARY_HALF) {
+      if (turns) v1 = rotate_pair8(v0, v1, cs_s + u * 64 + c0);
+    } else {
+      v0 = rotate_piece(v0, cs_s + u * 64, c0 / 2, a.pairs);
+      v1 = rotate_piece(v1, cs_s + u * 64, c1 / 2, a.pairs);
+    }
+    *reinterpret_cast<uint4*>(dst + c0) = v0;
+    *reinterpret_cast<uint4*>(dst + c1) = v1;
+  }
+}
+
+// Half layout with any even rotary_dim: a wave per row, lane i turns pair i and copies channels behind the pairs.  Both
+// channels of a pair belong to one lane, so a row may be turned in place.
+__global__ __launch_bounds__(kThreads) void rotary_any_kernel(const RotaryArgs a) {
+  const uint32_t l = blockIdx.y, row = blockIdx.x * (kThreads / kWave) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const uint32_t t = a.div_h.quot(row), h = row - t * a.H;
+  if (t >= a.T) return;
+  const uint16_t* src = a.x + static_cast<int64_t>(l) * a.x_sl + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
+  uint16_t* dst = a.out + static_cast<int64_t>(l) * a.o_sl + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
+  const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
+  if (lane < a.pairs) {
+    float p = __uint_as_float(static_cast<uint32_t>(src[lane]) << 16), q = __uint_as_float(static_cast<uint32_t>(src[lane + a.pairs]) << 16);
+    rotate(p, q, turn_of(a, pos, a.freq[lane]));
+    const uint32_t w = pack_bf16x2(p, q);
+    dst[lane] = static_cast<uint16_t>(w);
+    dst[lane + a.pairs] = static_cast<uint16_t>(w >> 16);
+  }
+  if (a.copy)
+    for (uint32_t c = 2 * a.pairs + lane; c < kHeadDim; c += kWave) dst[c] = src[c];
+}
+
+}  // namespace
+}  // namespace kvp
+
+extern "C" int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int32_t* positions, int64_t pos_stride_l,
+                              int64_t pos_stride_t, int64_t pos_stride_h, const double* freq, int32_t rotary_dim, int32_t layout,
+                              int32_t inverse, float mscale, void* stream) {
+  using namespace kvp;
+  int32_t rc = check_view(x);
+  if (rc == KVP_OK) rc = check_view(out);
+  if (rc != KVP_OK) return rc;
+  if (!positions || !freq) return KVP_ERR_NULL;
+  if (layout != KVP_ROTARY_HALF && layout != KVP_ROTARY_INTERLEAVED) return KVP_ERR_UNSUPPORTED;
+  if (rotary_dim < 2 || rotary_dim > kHeadDim || rotary_dim % 2) return KVP_ERR_UNSUPPORTED;
+  if (out->L != x->L || out->T != x->T || out->H != x->H) return KVP_ERR_SHAPE;
+  if (out->ptr == x->ptr && (out->stride_l != x->stride_l || out->stride_t != x->stride_t || out->stride_h != x->stride_h)) return KVP_ERR_SHAPE;
+  if (x->L > 65535 || x->T >= (1ll << 31) || x->H >= (1ll << 31) || x->T * x->H >= (1ll << 31)) return KVP_ERR_SHAPE;
+  if (pos_stride_l < 0 || pos_stride_t < 0 || pos_stride_h < 0) return KVP_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(freq) & 7u)) return KVP_ERR_ALIGN;
+  RotaryArgs a{};
+  a.x = static_cast<const uint16_t*>(x->ptr);
+  a.out = static_cast<uint16_t*>(const_cast<void*>(out->ptr));
+  a.x_sl = x->stride_l; a.x_st = x->stride_t; a.x_sh = x->stride_h;
+  a.o_sl = out->stride_l; a.o_st = out->stride_t; a.o_sh = out->stride_h;
+  a.pos = positions;
+  a.p_sl = pos_stride_l; a.p_st = pos_stride_t; a.p_sh = pos_stride_h;
+  a.freq = freq;
+  a.T = static_cast<uint32_t>(x->T);
+  a.H = static_cast<uint32_t>(x->H);
+  a.pairs = static_cast<uint32_t>(rotary_dim / 2);
+  a.div_h = FastDiv(a.H);
+  a.div_pairs = FastDiv(a.pairs);
+  a.mscale = mscale;
+  a.sign = inverse ? -1.0f : 1.0f;
+  a.copy = x->ptr != out->ptr;
+  const hipStream_t st = as_stream(stream);
+  const unsigned layers = static_cast<unsigned>(x->L);
+  if (layout == KVP_ROTARY_HALF && rotary_dim % 16) {
+    const int64_t rows = x->T * x->H;
+    rotary_any_kernel<<<dim3(static_cast<unsigned>(ceil_div(rows, kThreads / kWave)), layers), kThreads, 0, st>>>(a);
+    return launch_status();
+  }
+  a.unit_heads = pos_stride_h == 0 ? a.H : 1;
+  a.units = pos_stride_h == 0 ? a.T : a.T * a.H;
+  a.units_block = static_cast<uint32_t>(std::min<int64_t>(kMaxTokens, std::max<int64_t>(1, 128 / a.unit_heads)));
+  const dim3 grid(static_cast<unsigned>(ceil_div(a.units, a.units_block)), layers);
+  if (layout == KVP_ROTARY_HALF)
+    rotary_kernel<KVP_ROTARY_HALF><<<grid, kThreads, 0, st>>>(a);
+  else
+    rotary_kernel<KVP_ROTARY_INTERLEAVED><<<grid, kThreads, 0, st>>>(a);
+  return launch_status();
+}
+
+extern "C" int32_t kvp_rotary_frequencies(double base, int32_t rotary_dim, int32_t scaling, double factor, double original, double low,
+                                          double high, double* freq, float* mscale) {
+  using namespace kvp;
+  if (rotary_dim < 2 || rotary_dim > kHeadDim || rotary_dim % 2) return KVP_ERR_UNSUPPORTED;
+  if (scaling < KVP_ROTARY_PLAIN || scaling > KVP_ROTARY_BANDED) return KVP_ERR_UNSUPPORTED;
+  if (!(base > 1.0) || !isfinite(base)) return KVP_ERR_SHAPE;
+  if (scaling != KVP_ROTARY_PLAIN && !(factor >= 1.0 && isfinite(factor))) return KVP_ERR_SHAPE;
+  if (scaling == KVP_ROTARY_NTK && rotary_dim == 2) return KVP_ERR_SHAPE;
+  if (scaling >= KVP_ROTARY_YARN && !(original > 0.0 && isfinite(original) && low > 0.0 && high > low && isfinite(high))) return KVP_ERR_SHAPE;
+  if (mscale) *mscale = scaling == KVP_ROTARY_YARN ? static_cast<float>(0.1 * log(factor) + 1.0) : 1.0f;
+  if (!freq) return KVP_OK;
+  const double dim = rotary_dim, two_pi = 6.283185307179586;
+  if (scaling == KVP_ROTARY_NTK) base *= pow(factor, dim / (dim - 2.0));
+  const int32_t n = rotary_dim / 2;
+  // pair index at which the original context holds r turns: f = base^(-2 i / dim) = 2 pi r / original
+  auto index_of = [&](double r) { return dim * log(original / (two_pi * r)) / (2.0 * log(base)); };
+  double from = 0.0, to = 1.0;
+  if (scaling == KVP_ROTARY_YARN) {
+    from = fmin(fmax(floor(index_of(high)), 0.0), dim - 1.0);
+    to = fmin(fmax(ceil(index_of(low)), 0.0), dim - 1.0);
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    const double f = pow(base, -2.0 * i / dim);
+    double keep = 1.0;   // share of the unscaled frequency
+    if (scaling == KVP_ROTARY_LINEAR) {
+      keep = 0.0;
+    } else if (scaling == KVP_ROTARY_YARN) {
+      keep = to > from ? 1.0 - fmin(fmax((i - from) / (to - from), 0.0), 1.0) : (i <= from ? 1.0 : 0.0);
+    } else if (scaling == KVP_ROTARY_BANDED) {
+      keep = fmin(fmax((original * f / two_pi - low) / (high - low), 0.0), 1.0);
+    }
+    freq[i] = scaling == KVP_ROTARY_PLAIN || scaling == KVP_ROTARY_NTK ? f : keep * f + (1.0 - keep) * f / factor;
+  }
+  return KVP_OK;
+}

@@ -6,6 +6,7 @@ kernel launch happens inside the C library.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Iterable, Sequence
@@ -50,6 +51,12 @@ class _PolicyOp(ctypes.Structure):
 class _Dims(ctypes.Structure):
     _fields_ = [("L", _i64), ("Hkv", _i64), ("Hq", _i64), ("W", _i64), ("T", _i64), ("n_rows", _i64), ("k", _i64),
                 ("n_cfgs", _i32), ("method", _i32)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_codes", _vp), ("v_codes", _vp), ("k_scales", _vp), ("v_scales", _vp), ("block_table", _vp), ("lens", _vp),
+                ("B", _i64), ("num_blocks", _i64), ("bs", _i64), ("H", _i64), ("D", _i64), ("max_blocks", _i64),
+                ("table_stride", _i64), ("format", _i32)]
 
 
 class _Config(ctypes.Structure):
@@ -101,6 +108,22 @@ def _load(path: str = _LIB_PATH):
     lib.kvp_policy_insert.restype = _i32
     lib.kvp_policy_insert.argtypes = [_i32, _i32, _vp, _vp, _vp, P(_Tier), _i32, ctypes.c_double, _vp, _vp, _i32,
                                       P(_PolicyOp), _i32, P(_i32)]
+    lib.kvp_cache_append.restype = _i32
+    lib.kvp_cache_append.argtypes = [P(_Cache), P(_View), P(_View), _vp, _vp]
+    lib.kvp_cache_read.restype = _i32
+    lib.kvp_cache_read.argtypes = [P(_Cache), _vp, P(_View), P(_View), _vp]
+    lib.kvp_cache_attend.restype = _i32
+    lib.kvp_cache_attend.argtypes = [P(_View), P(_Cache), _vp, _i32, ctypes.c_float, P(_View), _vp, _vp, _i64, _i64, _vp, _sz, _vp]
+    lib.kvp_cache_attend_workspace_bytes.restype = _sz
+    lib.kvp_cache_attend_workspace_bytes.argtypes = [_i64] * 5 + [_i32]
+    lib.kvp_cache_evict.restype = _i32
+    lib.kvp_cache_evict.argtypes = [P(_Cache), _vp, _i64, _i64, _i64, _i64, P(_Cache), _vp, _vp, _i64, _vp, _i64, _vp, _sz, _vp]
+    lib.kvp_cache_evict_workspace_bytes.restype = _sz
+    lib.kvp_cache_evict_workspace_bytes.argtypes = [_i64] * 4
+    lib.kvp_rotary.restype = _i32
+    lib.kvp_rotary.argtypes = [P(_View), P(_View), _vp, _i64, _i64, _i64, _vp, _i32, _i32, _i32, ctypes.c_float, _vp]
+    lib.kvp_rotary_frequencies.restype = _i32
+    lib.kvp_rotary_frequencies.argtypes = [ctypes.c_double, _i32, _i32] + [ctypes.c_double] * 4 + [_vp, P(ctypes.c_float)]
     lib.kvp_workspace_bytes.restype = _sz
     lib.kvp_workspace_bytes.argtypes = [_i32, P(_Dims)]
     lib.kvp_keep_count.restype = _i64
@@ -147,6 +170,34 @@ class PagedKV:
     pool: torch.Tensor
     block_table: torch.Tensor
     T: int
+
+
+@dataclass
+class KVCache:
+    """8-bit paged cache of one layer: k_codes u8 [num_blocks][H][bs][D], v_codes u8 [num_blocks][H][D][bs], k_scales and
+    v_scales f32 [num_blocks][H], block_table int32 [B][max_blocks], lens int32 [B], fmt "int8" or "e4m3"."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+    block_table: torch.Tensor
+    lens: torch.Tensor
+    fmt: str = "int8"
+
+    @property
+    def bs(self) -> int:
+        return self.k_codes.shape[2]
+
+    def nbytes(self) -> int:
+        return 2 * self.k_codes.numel() + 8 * self.k_scales.numel()
+
+
+def alloc_cache(num_blocks: int, H: int, D: int, bs: int, block_table: torch.Tensor, lens: torch.Tensor, fmt: str = "int8") -> KVCache:
+    """A cache of the sequences that block_table [B][max_blocks] and lens [B] describe, over a pool of its own."""
+    dev = block_table.device
+    codes = [torch.empty(shape, dtype=torch.uint8, device=dev) for shape in ((num_blocks, H, bs, D), (num_blocks, H, D, bs))]
+    scales = [torch.empty(num_blocks, H, dtype=torch.float32, device=dev) for _ in range(2)]
+    return KVCache(*codes, *scales, block_table, lens, fmt)
 
 
 def alloc_qplane(L: int, T: int, H: int, D: int, bits: int, group: int, device, page: int = 16,
@@ -263,6 +314,80 @@ def _qplane(q: QPlane) -> _QPlane:
     return v
 
 
+KVP_CACHE_INT8, KVP_CACHE_E4M3 = 0, 1
+_CACHE_FORMATS = {"int8": KVP_CACHE_INT8, "e4m3": KVP_CACHE_E4M3}
+
+
+def _cache(c: KVCache) -> _Cache:
+    # like _paged: the marshalled struct is kept, keyed by everything it is made of
+    ts = (c.k_codes, c.v_codes, c.k_scales, c.v_scales, c.block_table, c.lens)
+    key = (c.fmt, *[t.data_ptr() for t in ts], c.k_codes.shape, c.v_codes.shape, c.k_scales.shape, c.v_scales.shape, c.block_table.shape,
+           c.block_table.stride(), c.lens.shape, c.k_codes.stride(), c.v_codes.stride())
+    kept = c.__dict__.get("_c")
+    if kept is not None and kept[0] == key:
+        return kept[1]
+    if c.fmt not in _CACHE_FORMATS:
+        raise ValueError('fmt must be "int8" or "e4m3"')
+    if c.k_codes.dtype != torch.uint8 or c.v_codes.dtype != torch.uint8 or c.k_codes.dim() != 4:
+        raise ValueError("codes must be uint8 [num_blocks][H][bs][D] and [num_blocks][H][D][bs]")
+    NB, H, bs, D = c.k_codes.shape
+    if tuple(c.v_codes.shape) != (NB, H, D, bs):
+        raise ValueError("v_codes must be [num_blocks][H][D][bs]")
+    for s in (c.k_scales, c.v_scales):
+        if s.dtype != torch.float32 or tuple(s.shape) != (NB, H) or not s.is_contiguous():
+            raise ValueError("scales must be contiguous float32 [num_blocks][H]")
+    if not (c.k_codes.is_contiguous() and c.v_codes.is_contiguous()):
+        raise ValueError("codes must be contiguous")
+    t = c.block_table
+    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("block_table must be int32 [B][max_blocks] with contiguous rows")
+    if c.lens.dtype != torch.int32 or tuple(c.lens.shape) != (t.shape[0],) or not c.lens.is_contiguous():
+        raise ValueError("lens must be contiguous int32 [B]")
+    _one_device(*ts)
+    v = _Cache(*[x.data_ptr() for x in ts], t.shape[0], NB, bs, H, D, t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1],
+               _CACHE_FORMATS[c.fmt])
+    c.__dict__["_c"] = (key, v)
+    return v
+
+
+def _one_device(first, *ts):
+    _need_cuda(first, *ts)
+    d = first.get_device()
+    for t in ts:
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors of one call must live on one device")
+
+
+def _per_sequence(t, B: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 [B]")
+    return t.data_ptr()
+
+
+def _weight_rows(t, B: int, H: int, n: int, what: str):
+    """(pointer, row stride) of float32 [B][H][>= n] whose B * H rows are equally far apart."""
+    if t.dtype != torch.float32 or t.dim() != 3 or tuple(t.shape[:2]) != (B, H) or t.shape[2] < n or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what} must be float32 [B][H][n] with contiguous rows of at least {n} entries")
+    stride = t.stride(1) if H > 1 else t.stride(0) if B > 1 else t.shape[2]
+    if B > 1 and H > 1 and t.stride(0) != H * t.stride(1):
+        raise ValueError(f"the rows of {what} must be equally far apart")
+    return t.data_ptr(), stride
+
+
+def _launch(like: torch.Tensor, stream, what: str, fn, *args):
+    """Runs a C entry point with the device of `like` current and its current stream, or the given one."""
+    d = like.get_device()
+    if d == torch.cuda.current_device():
+        rc = fn(*args, _stream(stream, like))
+    else:
+        with torch.cuda.device(d):
+            rc = fn(*args, _stream(stream, like))
+    if rc != 0:
+        raise KVPError(rc, what)
+
+
 def _check(rc: int, what: str):
     if rc != 0:
         raise KVPError(rc, what)
@@ -301,6 +426,7 @@ def kvp_version() -> int:
 
 
 KVP_WS_SCORE_TOKENS, KVP_WS_SCORE_KEYS, KVP_WS_SELECT_TOPK, KVP_WS_EVAL_CONFIGS = 0, 1, 2, 3
+KVP_WS_CACHE_ATTEND, KVP_WS_CACHE_EVICT = 4, 5
 
 
 def kvp_workspace_bytes(op: int, L: int = 0, Hkv: int = 0, Hq: int = 0, W: int = 0, T: int = 0, n_rows: int = 0,
@@ -529,6 +655,138 @@ def kvp_policy_insert(nbytes, quality, frequency, tiers, alpha: float, ctx_tier,
                                 ctypes.byref(n))
     _check(rc, "kvp_policy_insert")
     return [(o.ctx, o.cfg, o.tier, o.op) for o in ops[: n.value]]
+
+
+# ------------------------------------------------------------------ the 8-bit paged cache and rotary positions
+
+def kvp_cache_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, counts: torch.Tensor | None = None, stream=None) -> KVCache:
+    """k, v bf16 [B][W][H][D]: rows w < counts[b] (int32 [B]; None: all) become tokens lens[b] + w.  lens is not changed."""
+    cs = _cache(cache)
+    _one_device(cache.k_codes, k, v, counts)
+    _launch(cache.k_codes, stream, "kvp_cache_append", _lib.kvp_cache_append, ctypes.byref(cs), ctypes.byref(_view(k)),
+            ctypes.byref(_view(v)), _per_sequence(counts, cs.B, "counts"))
+    return cache
+
+
+def kvp_cache_read(cache: KVCache, k_out: torch.Tensor | None, v_out: torch.Tensor | None = None, first: torch.Tensor | None = None,
+                   stream=None):
+    """Tokens first[b] + i (int32 [B]; None: 0) of every sequence restored to rows i of k_out, v_out, bf16 [B][R][H][D]; rows
+    behind the last token are left as they were.  Returns (k_out, v_out)."""
+    cs = _cache(cache)
+    _one_device(cache.k_codes, k_out, v_out, first)
+    _launch(cache.k_codes, stream, "kvp_cache_read", _lib.kvp_cache_read, ctypes.byref(cs), _per_sequence(first, cs.B, "first"),
+            ctypes.byref(_view(k_out)) if k_out is not None else None, ctypes.byref(_view(v_out)) if v_out is not None else None)
+    return k_out, v_out
+
+
+def kvp_cache_attend_workspace_bytes(B: int, H: int, Hq: int, W: int, max_len: int, weights: bool = False) -> int:
+    return int(_lib.kvp_cache_attend_workspace_bytes(B, H, Hq, W, max_len, int(weights)))
+
+
+def kvp_cache_attend(q: torch.Tensor, cache: KVCache, out: torch.Tensor | None = None, q_lens: torch.Tensor | None = None,
+                     causal: bool = True, scale: float | None = None, acc_in: torch.Tensor | None = None,
+                     acc_out: torch.Tensor | None = None, max_len: int = 0, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of q bf16 [B][W][Hq][D] over the cache -> out of the same shape; the q_lens[b] (int32 [B]; None: W) query tokens of a
+    sequence are its last ones.  scale: 1 / sqrt(D) if None.  acc_out f32 [B][H][>= max_len] receives acc_in (or 0) plus the weight
+    that every token drew.  max_len: an upper bound of lens, 0 for the capacity.  Rows behind q_lens[b] are not written."""
+    cs = _cache(cache)
+    if out is None:
+        out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+    _one_device(cache.k_codes, q, out, q_lens, acc_in, acc_out, ws)
+    qv, ov = _view(q), _view(out)
+    cap = cs.max_blocks * cs.bs
+    n = cap if max_len == 0 else min(max_len, cap)
+    ai = ao = None
+    stride = 0
+    if acc_out is not None:
+        ao, stride = _weight_rows(acc_out, cs.B, cs.H, n, "acc_out")
+        if acc_in is not None:
+            ai, stride_in = _weight_rows(acc_in, cs.B, cs.H, n, "acc_in")
+            if stride_in != stride:
+                raise ValueError("acc_in and acc_out must have the same strides")
+    elif acc_in is not None:
+        raise ValueError("acc_in is given without acc_out")
+    need = 0 if ws is not None else kvp_cache_attend_workspace_bytes(cs.B, cs.H, qv.H, qv.T, n, acc_out is not None)
+    ws, wp, wb = _workspace(ws, need, q.device, stream)
+    _launch(q, stream, "kvp_cache_attend", _lib.kvp_cache_attend, ctypes.byref(qv), ctypes.byref(cs), _per_sequence(q_lens, cs.B, "q_lens"),
+            int(causal), 1.0 / math.sqrt(qv.D) if scale is None else float(scale), ctypes.byref(ov), ai, ao, stride, max_len, wp, wb)
+    return out
+
+
+def kvp_cache_evict_workspace_bytes(B: int, H: int, max_len: int, budget: int) -> int:
+    return int(_lib.kvp_cache_evict_workspace_bytes(B, H, max_len, budget))
+
+
+def kvp_cache_evict(src: KVCache, acc: torch.Tensor, budget: int, dst: KVCache, sink: int = 0, recent: int = 0,
+                    keep_idx: torch.Tensor | None = None, acc_out: torch.Tensor | None = None, lens_out: torch.Tensor | None = None,
+                    max_len: int = 0, ws: torch.Tensor | None = None, stream=None) -> KVCache:
+    """Keeps `budget` tokens of every (sequence, head) of src: the first `sink`, the last `recent` and those of the largest acc f32
+    [B][H][>= max_len], and moves them to the pages of dst (other pages than those of src).  keep_idx int32 [B][H][budget]: the
+    old indices, -1 behind the last; acc_out f32 [B][H][>= budget]: the kept weights; lens_out int32 [B] (dst.lens, say): the new lengths."""
+    ss, ds = _cache(src), _cache(dst)
+    _one_device(src.k_codes, dst.k_codes, acc, keep_idx, acc_out, lens_out, ws)
+    cap = ss.max_blocks * ss.bs
+    n = cap if max_len == 0 else min(max_len, cap)
+    ap, a_stride = _weight_rows(acc, ss.B, ss.H, n, "acc")
+    op, o_stride = (None, 0) if acc_out is None else _weight_rows(acc_out, ss.B, ss.H, budget, "acc_out")
+    kp = None
+    if keep_idx is not None:
+        if keep_idx.dtype != torch.int32 or not keep_idx.is_contiguous() or tuple(keep_idx.shape) != (ss.B, ss.H, budget):
+            raise ValueError("keep_idx must be contiguous int32 [B][H][budget]")
+        kp = keep_idx.data_ptr()
+    need = 0 if ws is not None else kvp_cache_evict_workspace_bytes(ss.B, ss.H, n, budget)
+    ws, wp, wb = _workspace(ws, need, acc.device, stream)
+    _launch(acc, stream, "kvp_cache_evict", _lib.kvp_cache_evict, ctypes.byref(ss), ap, a_stride, budget, sink, recent, ctypes.byref(ds), kp,
+            op, o_stride, _per_sequence(lens_out, ss.B, "lens_out"), max_len, wp, wb)
+    return dst
+
+
+KVP_ROTARY_HALF, KVP_ROTARY_INTERLEAVED = 0, 1
+KVP_ROTARY_PLAIN, KVP_ROTARY_LINEAR, KVP_ROTARY_NTK, KVP_ROTARY_YARN, KVP_ROTARY_BANDED = 0, 1, 2, 3, 4
+_ROTARY_LAYOUTS = {"half": KVP_ROTARY_HALF, "interleaved": KVP_ROTARY_INTERLEAVED}
+_ROTARY_SCALINGS = {"plain": KVP_ROTARY_PLAIN, "linear": KVP_ROTARY_LINEAR, "ntk": KVP_ROTARY_NTK, "yarn": KVP_ROTARY_YARN,
+                    "banded": KVP_ROTARY_BANDED}
+
+
+def kvp_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original: float = 0.0,
+                           low: float = 1.0, high: float = 32.0):
+    """Host call.  (freq float64 cpu tensor [rotary_dim / 2], mscale) for a context `factor` times as long as the `original` one;
+    scaling: plain, linear, ntk, yarn, banded."""
+    if scaling not in _ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(_ROTARY_SCALINGS)}")
+    freq = torch.empty(max(rotary_dim // 2, 1), dtype=torch.float64)
+    m = ctypes.c_float(0.0)
+    _check(_lib.kvp_rotary_frequencies(float(base), int(rotary_dim), _ROTARY_SCALINGS[scaling], float(factor), float(original), float(low),
+                                       float(high), freq.data_ptr(), ctypes.byref(m)), "kvp_rotary_frequencies")
+    return freq, float(m.value)
+
+
+def kvp_rotary(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, out: torch.Tensor | None = None, layout: str = "half",
+               inverse: bool = False, mscale: float = 1.0, stream=None) -> torch.Tensor:
+    """Turns the pairs of the first 2 * len(freq) channels of x bf16 [L][T][H][D] by position * freq (float64, radians).
+    positions int32: [T], [L][T], or [L][H][T] as a keep list is laid out.  out may be x."""
+    if layout not in _ROTARY_LAYOUTS:
+        raise ValueError('layout must be "half" or "interleaved"')
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    _one_device(x, out, positions, freq)
+    xv, ov = _view(x), _view(out)
+    if positions.dtype != torch.int32:
+        raise ValueError("positions must be int32")
+    shape, st = tuple(positions.shape), positions.stride()
+    if shape == (xv.T,):
+        sl, stt, sh = 0, st[0], 0
+    elif shape == (xv.L, xv.T):
+        sl, stt, sh = st[0], st[1], 0
+    elif shape == (xv.L, xv.H, xv.T):
+        sl, stt, sh = st[0], st[2], st[1]
+    else:
+        raise ValueError("positions must be [T], [L][T] or [L][H][T]")
+    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError("freq must be contiguous float64 [rotary_dim / 2]")
+    _launch(x, stream, "kvp_rotary", _lib.kvp_rotary, ctypes.byref(xv), ctypes.byref(ov), positions.data_ptr(), sl, stt, sh, freq.data_ptr(),
+            2 * freq.shape[0], _ROTARY_LAYOUTS[layout], int(inverse), float(mscale))
+    return out
 
 
 def kvp_copy_bytes(dst: torch.Tensor, src: torch.Tensor, stream=None):

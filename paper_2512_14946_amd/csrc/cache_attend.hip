@@ -16,6 +16,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache_attend_plan.h"
 #include "cache_common.h"
 
@@ -30,7 +32,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;              // how far (base 2) a logit may exceed the reference of its row
 constexpr float kValueSlack = 64.0f;        // and a page's value scale the reference scale: 2^8 * 2^6 fits a half
 constexpr float kLeastScale = 0x1p-100f;    // value scales below this count as this one's fractions
+constexpr float kLeast = -3.402823466e38f;
+constexpr int kKeptFloats = 4096;           // logits that a wave keeps in LDS: 4 tiles of 16 rows, 8 of 8
 constexpr int kOutPitch = 132;              // floats per row of partial outputs in LDS
+constexpr uint32_t kSlice = 4 * kThreads;   // tokens of a block that sums weights from logits
 
 struct AttendArgs {
   CacheArgs c;
@@ -44,7 +49,9 @@ struct AttendArgs {
   int32_t causal;
   float* part_out;                          // [cell][chunk][16][128] unnormalized, or null (one chunk)
   float2* part_stat;                        // [cell][chunk][16] (reference, sum)
-  float2* row_stat;                         // [cell][16] (reference, 1 / sum), or null (no weights asked for)
+  float2* row_stat;                         // [cell][16] (reference, 1 / sum): weights of more than one row tile
+  float* logits;                            // [cell][tile of 64 tokens][i][M][g][4], see the kernel: weights of a single row tile
+  int64_t logit_stride;
   const float* acc_in;
   float* acc_out;
   int64_t acc_stride;
@@ -81,7 +88,8 @@ __device__ __forceinline__ Rows rows_of(const AttendArgs& a, uint32_t cell) {
   return r;
 }
 
-// One query row as operands of the four channel steps: halves of q / 2^e, and what turns their products into base-2 logits.
+// One query row as operands of the four channel steps: halves of q / 2^e with the sign of the softmax scale, and the positive factor that turns
+// their products with codes into base-2 logits.
 // Step 2 jj + half of lane group g takes channels 64 jj + 16 g + 8 half ..+7, as the keys are loaded.
 __device__ __forceinline__ float load_query(const uint16_t* row, int g, bool valid, float scale2, half8_t qf[4]) {
   uint4 raw[4];
@@ -99,17 +107,26 @@ __device__ __forceinline__ float load_query(const uint16_t* row, int g, bool val
   top = fmaxf(top, __shfl_xor(top, 16));
   top = fmaxf(top, __shfl_xor(top, 32));
   const int e = __builtin_amdgcn_frexp_expf(top);   // 0 for a zero row
+  const float sign = scale2 < 0.0f ? -1.0f : 1.0f;
 #pragma unroll
   for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) qf[s][i] = static_cast<_Float16>(ldexpf(x[s][i], -e));
-  return ldexpf(scale2, e);
+    for (int i = 0; i < 8; ++i) qf[s][i] = static_cast<_Float16>(ldexpf(x[s][i] * sign, -e));
+  return ldexpf(fabsf(scale2), e);
 }
 
-// Pool page of the 16-token run that starts at token t; runs behind the last token take its page.
-__device__ __forceinline__ int64_t run_cell(const AttendArgs& a, uint32_t b, uint32_t h, uint32_t t, uint32_t n) {
-  return static_cast<int64_t>(cache_page(a.c, b, min(t, n - 1) >> a.c.bs_log2)) * a.c.H + h;
+// Table entry of the 16-token run that starts at token t, and the pool cell that it names; runs behind the last token take its page.
+__device__ __forceinline__ int32_t run_entry(const AttendArgs& a, uint32_t b, uint32_t t, uint32_t n) {
+  return a.c.table[static_cast<int64_t>(b) * a.c.table_stride + (min(t, n - 1) >> a.c.bs_log2)];
 }
+__device__ __forceinline__ int64_t entry_cell(const AttendArgs& a, uint32_t h, int32_t entry) {
+  return static_cast<int64_t>(clamp_page(a.c, entry)) * a.c.H + h;
+}
+__device__ __forceinline__ int64_t run_cell(const AttendArgs& a, uint32_t b, uint32_t h, uint32_t t, uint32_t n) {
+  return entry_cell(a, h, run_entry(a, b, t, n));
+}
+
+__device__ __forceinline__ uint32_t run_k_of(uint32_t t, int col) { return t + 16 * (col >> 2); }
 
 // Keys of 64 tokens: row r of product j is token 16 (r / 4) + 4 j + r mod 4, so that lane group g ends up with tokens 16 g ..+15
 __device__ __forceinline__ void load_keys(const AttendArgs& a, int64_t cell, uint32_t t_run, int lane, uint4 k[4][2]) {
@@ -118,13 +135,13 @@ __device__ __forceinline__ void load_keys(const AttendArgs& a, int64_t cell, uin
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int jj = 0; jj < 2; ++jj) k[j][jj] = *reinterpret_cast<const uint4*>(p + 4 * j * kHeadDim + 64 * jj);
+    for (int jj = 0; jj < 2; ++jj) k[j][jj] = load_stream16(p + 4 * j * kHeadDim + 64 * jj);
 }
 __device__ __forceinline__ void load_values(const AttendArgs& a, int64_t cell, uint32_t t_run, int lane, uint4 v[8]) {
   const uint32_t slot = t_run & ((1u << a.c.bs_log2) - 1);
   const uint8_t* p = a.c.v_codes + (cell << (a.c.bs_log2 + 7)) + (static_cast<uint32_t>(lane & 15) << a.c.bs_log2) + slot;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) v[c] = *reinterpret_cast<const uint4*>(p + (static_cast<uint32_t>(16 * c) << a.c.bs_log2));
+  for (int c = 0; c < 8; ++c) v[c] = load_stream16(p + (static_cast<uint32_t>(16 * c) << a.c.bs_log2));
 }
 
 template <int FMT>
@@ -140,9 +157,10 @@ __device__ __forceinline__ void logits(const uint4 k[4][2], const half8_t qf[4],
   }
 }
 
-template <int FMT>
+template <int FMT, bool LOGITS>
 __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs a) {
-  __shared__ __attribute__((aligned(16))) float out_s[kWaves][kTileRows * kOutPitch];
+  constexpr int kOutFloats = kTileRows * kOutPitch;
+  __shared__ __attribute__((aligned(16))) float shared_s[kWaves * (LOGITS ? kKeptFloats : kOutFloats)];   // kept logits, then the waves' results
   __shared__ float ref_s[kWaves][kTileRows], sum_s[kWaves][kTileRows], val_s[kWaves];
   const uint32_t cell = a.div_chunks.quot(blockIdx.x), chunk = blockIdx.x - cell * a.chunks;
   const Rows r = rows_of(a, cell);
@@ -158,26 +176,54 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
                               valid, a.scale2, qf);
   const uint32_t limit = valid ? seen_by(a, r.n, r.m, w) : 0u;
 
+  // Logits kept for the weights leave by way of LDS, some tiles at a time: loads that a wave requests after a store wait for that
+  // store too, and a few stores in every tile cost 129 us of 409 at 64 x 8 x 12288 tokens and 8 rows.
+  float* kept_s = reinterpret_cast<float*>(shared_s) + wave * kKeptFloats;
+  const uint32_t keep = kKeptFloats / (a.M * kTileTokens);
+  uint32_t n_kept = 0;
+
   floatx4 o[8];
 #pragma unroll
   for (int c = 0; c < 8; ++c) o[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  float ref = -3.402823466e38f, sum = 0.0f, vref = kLeastScale;
+  float ref = kLeast, sum = 0.0f, vref = kLeastScale, inv_vref = 1.0f / kLeastScale;
 
-  for (uint32_t t = t0 + wave * kTileTokens; t < t1; t += kWaves * kTileTokens) {
-    const uint32_t run_k = t + 16 * (col >> 2), run = t + 16 * g;   // the runs this lane's keys and its tokens lie in
-    uint4 k[4][2], v[8];
-    load_keys(a, run_cell(a, r.b, r.h, run_k, r.n), run_k, lane, k);
-    const int64_t cell_v = run_cell(a, r.b, r.h, run, r.n);
-    load_values(a, cell_v, run, lane, v);
-    const float f = a.c.k_scales[cell_v] * qs, vs = a.c.v_scales[cell_v];
+  // The keys of the next tile are requested when this tile's are used up, its values likewise, with the scales and the table entries
+  // of the tile after it in between: one set of registers, loads in flight all the time, and none waited for before its turn.
+  constexpr uint32_t kStep = kTileTokens;
+  const uint32_t part_tokens = (t1 > t0 ? (t1 - t0 + kWaves * kTileTokens - 1) / (kWaves * kTileTokens) : 0u) * kTileTokens;   // tokens of a wave
+  uint32_t t = t0 + wave * part_tokens;
+  const uint32_t t_end = min(t1, t + part_tokens);
+  uint4 k[4][2], v[8];
+  float ks, vs;
+  int32_t entry_k = 0, entry_v = 0;
+  if (t < t_end) {
+    const int64_t cell_k = run_cell(a, r.b, r.h, run_k_of(t, col), r.n), cell_v = run_cell(a, r.b, r.h, t + 16 * g, r.n);
+    load_keys(a, cell_k, run_k_of(t, col), lane, k);
+    ks = a.c.k_scales[cell_v];
+    vs = a.c.v_scales[cell_v];
+    entry_k = run_entry(a, r.b, run_k_of(t + kStep, col), r.n);
+    entry_v = run_entry(a, r.b, t + kStep + 16 * g, r.n);
+    load_values(a, cell_v, t + 16 * g, lane, v);
+  }
+  // MORE is known at compile time: behind a branch around the loads, every wait would have to count them as not issued.
+  auto tile = [&](auto more_tag) {
+    constexpr bool MORE = decltype(more_tag)::value;
+    const uint32_t run = t + 16 * g;       // the 16 tokens of this lane
+    const float f = fmaxf(ks * qs, 0x1p-126f), vs_now = vs;   // never 0: what is masked stays -inf
     floatx4 s[4];
     logits<FMT>(k, qf, s);
-    float x[16], top;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = s[i >> 2][i & 3] * f;
+    int64_t cell_v = 0;
+    if constexpr (MORE) {
+      cell_v = entry_cell(a, r.h, entry_v);
+      load_keys(a, entry_cell(a, r.h, entry_k), run_k_of(t + kStep, col), lane, k);
+      ks = a.c.k_scales[cell_v];
+      vs = a.c.v_scales[cell_v];
+      entry_k = run_entry(a, r.b, run_k_of(t + 2 * kStep, col), r.n);
+      entry_v = run_entry(a, r.b, run + 2 * kStep, r.n);
+    }
     if (t + kTileTokens > r.least) {         // some row does not see the whole tile
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = run + i < limit ? x[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[i >> 2][i & 3] = run + i < limit ? s[i >> 2][i & 3] : -INFINITY;
       if (t + kTileTokens > r.n) {           // bytes behind the last token may be anything: 0 * NaN is not 0
         const int live = static_cast<int>(min(max(static_cast<int64_t>(r.n) - run, int64_t(0)), int64_t(16)));
         uint32_t mask[4];
@@ -187,13 +233,23 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
         for (int c = 0; c < 8; ++c) v[c] = make_uint4(v[c].x & mask[0], v[c].y & mask[1], v[c].z & mask[2], v[c].w & mask[3]);
       }
     }
-    top = x[0];
+    if constexpr (LOGITS) {
+      // to LDS, as they lie in memory: [i][row][g][4]
+      if (col < static_cast<int>(a.M)) {
+        float4* to = reinterpret_cast<float4*>(kept_s) + (n_kept * 4 * a.M + col) * 4 + g;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-    if (__builtin_amdgcn_ballot_w64(top > ref + kSlack || vs > kValueSlack * vref)) {   // wave-uniform
+        for (int i = 0; i < 4; ++i) to[i * a.M * 4] = make_float4(s[i][0] * f, s[i][1] * f, s[i][2] * f, s[i][3] * f);
+      }
+      ++n_kept;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+    top *= f;                                // f > 0
+    if (__builtin_amdgcn_ballot_w64(top > ref + kSlack || vs_now > kValueSlack * vref)) {   // wave-uniform
       float ref_new = fmaxf(ref, fmaxf(top, __shfl_xor(top, 16)));
       ref_new = fmaxf(ref_new, __shfl_xor(ref_new, 32));
-      float v_new = fmaxf(vref, vs);
+      float v_new = fmaxf(vref, vs_now);
       v_new = fmaxf(v_new, __shfl_xor(v_new, 16));
       v_new = fmaxf(v_new, __shfl_xor(v_new, 32));
       const float down = __builtin_amdgcn_exp2f(ref - ref_new), down_o = down * (vref / v_new);
@@ -202,29 +258,47 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       for (int c = 0; c < 8; ++c) o[c] *= down_o;
       ref = ref_new;
       vref = v_new;
+      inv_vref = 1.0f / v_new;
     }
-    const float share = vs / vref;
-    float p[16];
+    // Probabilities times the page's share of the reference scale: the share goes into the exponent, and the sum of the tile is divided by it.
+    // A share below 2^-60 leaves nothing of a half either way, and a page of zeros has none: both count as 2^-60.
+    const float log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f), off = log_share - ref;
+    float p[16], part = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(x[i] - ref);
-      sum += p[i];
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], f, off));
+      part += p[i];
     }
+    sum = fmaf(part, __builtin_amdgcn_exp2f(-log_share), sum);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       half8_t pf;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pf[i] = static_cast<_Float16>(p[8 * half + i] * share);
+      for (int i = 0; i < 8; ++i) pf[i] = static_cast<_Float16>(p[8 * half + i]);
 #pragma unroll
       for (int c = 0; c < 8; ++c)
         o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half ? decode8_half<FMT>(v[c].z, v[c].w) : decode8_half<FMT>(v[c].x, v[c].y), pf, o[c], 0, 0, 0);
     }
-  }
+    if constexpr (MORE) load_values(a, cell_v, run + kStep, lane, v);
+    if constexpr (LOGITS) {
+      if (!MORE || n_kept == keep) {
+        float4* to = reinterpret_cast<float4*>(a.logits + static_cast<int64_t>(cell) * a.M * a.logit_stride + static_cast<int64_t>(t - (n_kept - 1) * kTileTokens) * a.M);
+        for (uint32_t i = lane; i < n_kept * a.M * 16; i += kWave) {
+          const float4 u = reinterpret_cast<const float4*>(kept_s)[i];
+          store_stream16(to + i, make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(u.z), __float_as_uint(u.w)));
+        }
+        n_kept = 0;
+      }
+    }
+  };
+  for (; t + kStep < t_end; t += kStep) tile(std::true_type{});
+  if (t < t_end) tile(std::false_type{});
+  if constexpr (LOGITS) __syncthreads();   // the waves' results go where others may still keep logits
 
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
 #pragma unroll
-  for (int c = 0; c < 8; ++c) *reinterpret_cast<floatx4*>(&out_s[wave][col * kOutPitch + 16 * c + 4 * g]) = o[c];
+  for (int c = 0; c < 8; ++c) *reinterpret_cast<floatx4*>(&shared_s[wave * kOutFloats + col * kOutPitch + 16 * c + 4 * g]) = o[c];
   if (g == 0) {
     ref_s[wave][col] = ref;
     sum_s[wave][col] = sum;
@@ -242,14 +316,15 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
     const float f = __builtin_amdgcn_exp2f(ref_s[i][orow] - m), fv = f * val_s[i];
     z = fmaf(sum_s[i][orow], f, z);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = fmaf(out_s[i][orow * kOutPitch + ch + j], fv, y[j]);
+    for (int j = 0; j < 8; ++j) y[j] = fmaf(shared_s[i * kOutFloats + orow * kOutPitch + ch + j], fv, y[j]);
   }
+  const int64_t at = (static_cast<int64_t>(cell) * a.chunks + chunk) * kTileRows + orow;
+  if (a.part_stat && ch == 0) a.part_stat[at] = make_float2(m, z);
   if (a.chunks > 1) {
-    const int64_t at = (static_cast<int64_t>(cell) * a.chunks + chunk) * kTileRows + orow;
+    if (r.tile * kTileRows + orow >= a.M) return;
     float4* dst = reinterpret_cast<float4*>(a.part_out + at * kHeadDim + ch);
     dst[0] = make_float4(y[0], y[1], y[2], y[3]);
     dst[1] = make_float4(y[4], y[5], y[6], y[7]);
-    if (ch == 0) a.part_stat[at] = make_float2(m, z);
     return;
   }
   const uint32_t r_out = r.tile * kTileRows + orow, w_out = a.div_g.quot(r_out);
@@ -262,34 +337,95 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
                                               pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
 }
 
-// The chunks of a row tile joined: a block per cell, thread -> (row, eight channels).
-__global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a) {
-  const uint32_t cell = blockIdx.x;
-  const Rows r = rows_of(a, cell);
-  const int orow = threadIdx.x >> 4, ch = (threadIdx.x & 15) * 8;
-  const uint32_t row = r.tile * kTileRows + orow, w = a.div_g.quot(row);
-  if (row >= a.M || static_cast<int32_t>(w) >= r.m) return;
-  const uint32_t n = (r.most + a.chunk - 1) / a.chunk;
-  const float2* st = a.part_stat + static_cast<int64_t>(cell) * a.chunks * kTileRows + orow;
-  const float* po = a.part_out + (static_cast<int64_t>(cell) * a.chunks * kTileRows + orow) * kHeadDim + ch;
-  float m = -3.402823466e38f;
-  for (uint32_t i = 0; i < n; ++i) m = fmaxf(m, st[i * kTileRows].x);
-  float z = 0.0f, y[8] = {};
-  for (uint32_t i = 0; i < n; ++i) {
-    const float2 s = st[i * kTileRows];
-    const float f = __builtin_amdgcn_exp2f(s.x - m);
-    z = fmaf(s.y, f, z);
-    const float4 u = *reinterpret_cast<const float4*>(po + static_cast<int64_t>(i) * kTileRows * kHeadDim);
-    const float4 v = *reinterpret_cast<const float4*>(po + static_cast<int64_t>(i) * kTileRows * kHeadDim + 4);
-    y[0] = fmaf(u.x, f, y[0]); y[1] = fmaf(u.y, f, y[1]); y[2] = fmaf(u.z, f, y[2]); y[3] = fmaf(u.w, f, y[3]);
-    y[4] = fmaf(v.x, f, y[4]); y[5] = fmaf(v.y, f, y[5]); y[6] = fmaf(v.z, f, y[6]); y[7] = fmaf(v.w, f, y[7]);
+// Row statistics over the chunks of a cell, by the 16 lanes that share `row`: (reference, 1 / sum); n chunks.
+__device__ __forceinline__ float2 joined_stats(const float2* st, uint32_t n, uint32_t lane16) {
+  float m = kLeast, z = 0.0f;
+  for (uint32_t i = lane16; i < n; i += 16) {
+    const float2 s = st[static_cast<int64_t>(i) * kTileRows];
+    const float m_new = fmaxf(m, s.x);
+    z = fmaf(z, __builtin_amdgcn_exp2f(m - m_new), s.y * __builtin_amdgcn_exp2f(s.x - m_new));
+    m = m_new;
   }
-  const float inv = z > 0.0f ? 1.0f / z : 0.0f;
-  if (a.row_stat && ch == 0) a.row_stat[static_cast<int64_t>(cell) * kTileRows + orow] = make_float2(m, inv);
-  uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw +
-                  static_cast<int64_t>(r.h * a.G + (row - w * a.G)) * a.o_sh + ch;
-  *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv),
-                                              pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) {
+    const float m2 = __shfl_xor(m, d), z2 = __shfl_xor(z, d), m_new = fmaxf(m, m2);
+    // written so that both lanes of an exchange form the same sum
+    const float lo = z * __builtin_amdgcn_exp2f(m - m_new), hi = z2 * __builtin_amdgcn_exp2f(m2 - m_new);
+    z = lo + hi;
+    m = m_new;
+  }
+  return make_float2(m, z > 0.0f ? 1.0f / z : 0.0f);
+}
+
+// The chunks of a row joined (blocks below n_join: one per row of a cell), and, with logits kept, what every token drew
+// (the other blocks: kSlice tokens of a cell each).  Both work out the final statistics of their rows from the chunks'.
+__global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a, uint32_t n_join, uint32_t join_rows, FastDiv div_rows, uint32_t slices,
+                                                              FastDiv div_slices) {
+  __shared__ __attribute__((aligned(16))) float4 part_s[8][32];
+  __shared__ float2 stat_s[kTileRows];
+  const uint32_t tid = threadIdx.x;
+  if (blockIdx.x < n_join) {
+    const uint32_t cell = div_rows.quot(blockIdx.x), orow = blockIdx.x - cell * join_rows;
+    const Rows r = rows_of(a, cell);
+    const uint32_t row = r.tile * kTileRows + orow, w = a.div_g.quot(row);
+    if (row >= a.M || static_cast<int32_t>(w) >= r.m) return;
+    const uint32_t n = (r.most + a.chunk - 1) / a.chunk;
+    const float2* st = a.part_stat + static_cast<int64_t>(cell) * a.chunks * kTileRows + orow;
+    const float2 stat = joined_stats(st, n, tid & 15);
+    if (a.row_stat && tid == 0) a.row_stat[static_cast<int64_t>(cell) * kTileRows + orow] = stat;
+    const uint32_t group = tid >> 5, ch = tid & 31;
+    const float4* po = reinterpret_cast<const float4*>(a.part_out + (static_cast<int64_t>(cell) * a.chunks * kTileRows + orow) * kHeadDim) + ch;
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (uint32_t i = group; i < n; i += 8) {
+      const float f = __builtin_amdgcn_exp2f(st[static_cast<int64_t>(i) * kTileRows].x - stat.x);
+      const float4 u = po[static_cast<int64_t>(i) * (kTileRows * kHeadDim / 4)];
+      y.x = fmaf(u.x, f, y.x); y.y = fmaf(u.y, f, y.y); y.z = fmaf(u.z, f, y.z); y.w = fmaf(u.w, f, y.w);
+    }
+    part_s[group][ch] = y;
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      const float4 u = part_s[i][ch];
+      y.x += u.x; y.y += u.y; y.z += u.z; y.w += u.w;
+    }
+    uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw +
+                    static_cast<int64_t>(r.h * a.G + (row - w * a.G)) * a.o_sh + ch * 4;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(y.x * stat.y, y.y * stat.y), pack_bf16x2(y.z * stat.y, y.w * stat.y));
+    return;
+  }
+  // one row tile per (sequence, head) here: a cell is a (sequence, head)
+  const uint32_t id = blockIdx.x - n_join, cell = div_slices.quot(id), t0 = (id - cell * slices) * kSlice;
+  const Rows r = rows_of(a, cell);
+  if (t0 >= r.n) return;
+  {
+    const uint32_t orow = tid >> 4, w = a.div_g.quot(orow);
+    float2 stat = make_float2(0.0f, 0.0f);
+    if (orow < a.M && static_cast<int32_t>(w) < r.m)
+      stat = joined_stats(a.part_stat + static_cast<int64_t>(cell) * a.chunks * kTileRows + orow, (r.most + a.chunk - 1) / a.chunk, tid & 15);
+    if ((tid & 15) == 0) stat_s[orow] = stat;
+  }
+  __syncthreads();
+  // 16 threads a tile, thread 4 i + g has tokens 16 g + 4 i ..+3
+  const uint32_t tile0 = t0 + (tid >> 4) * kTileTokens, t = tile0 + (tid & 3) * 16 + ((tid >> 2) & 3) * 4;
+  if (t >= r.n) return;
+  float drawn[4] = {};
+  if (tile0 < r.most) {   // a tile beyond what any row sees has no logits
+    const float* x = a.logits + static_cast<int64_t>(cell) * a.M * a.logit_stride + static_cast<int64_t>(tile0) * a.M + (((tid >> 2) & 3) * a.M * 4 + (tid & 3)) * 4;
+    for (uint32_t i = 0; i < a.M; ++i) {
+      const float4 u = *reinterpret_cast<const float4*>(x + i * 16);
+      const float2 stat = stat_s[i];
+      drawn[0] = fmaf(__builtin_amdgcn_exp2f(u.x - stat.x), stat.y, drawn[0]);
+      drawn[1] = fmaf(__builtin_amdgcn_exp2f(u.y - stat.x), stat.y, drawn[1]);
+      drawn[2] = fmaf(__builtin_amdgcn_exp2f(u.z - stat.x), stat.y, drawn[2]);
+      drawn[3] = fmaf(__builtin_amdgcn_exp2f(u.w - stat.x), stat.y, drawn[3]);
+    }
+  }
+  const int64_t at = static_cast<int64_t>(cell) * a.acc_stride + t;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+    if (t + i < r.n) a.acc_out[at + i] = (a.acc_in ? a.acc_in[at + i] : 0.0f) + drawn[i];
 }
 
 // What every token drew: a wave owns 64 tokens of a (sequence, head) and goes through all query rows that see them; its sums
@@ -358,7 +494,7 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   if (acc_out && acc_stride < max_len) return KVP_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(q_lens) | reinterpret_cast<uintptr_t>(acc_in) | reinterpret_cast<uintptr_t>(acc_out)) & 3u) return KVP_ERR_ALIGN;
   const AttendPlan p = make_attend_plan(cache->B, cache->H, q->H, W, max_len, acc_out != nullptr);
-  if (p.cells * p.chunks >= (1ll << 31)) return KVP_ERR_SHAPE;
+  if (p.cells * std::max<int64_t>(p.chunks, kTileRows) + p.cells * ceil_div(max_len, kSlice) >= (1ll << 31)) return KVP_ERR_SHAPE;
   if (p.bytes != 0 && (!ws || ws_bytes < p.bytes || !aligned16(ws))) return KVP_ERR_WORKSPACE;
   AttendArgs a{};
   a.c = cache_args(cache);
@@ -381,23 +517,28 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   a.scale2 = scale * kLog2e;
   a.causal = causal;
   char* w = static_cast<char*>(ws);
-  if (p.chunks > 1) {
-    a.part_out = reinterpret_cast<float*>(w);
-    a.part_stat = reinterpret_cast<float2*>(w + p.out_bytes);
-  }
+  if (p.out_bytes) a.part_out = reinterpret_cast<float*>(w);
+  if (p.stat_bytes) a.part_stat = reinterpret_cast<float2*>(w + p.out_bytes);
+  if (p.row_bytes) a.row_stat = reinterpret_cast<float2*>(w + p.out_bytes + p.stat_bytes);
+  if (p.logit_bytes) a.logits = reinterpret_cast<float*>(w + p.out_bytes + p.stat_bytes + p.row_bytes);
+  a.logit_stride = p.logit_stride;
   a.acc_in = acc_in;
   a.acc_out = acc_out;
   a.acc_stride = acc_stride;
-  if (acc_out) a.row_stat = reinterpret_cast<float2*>(w + p.out_bytes + p.stat_bytes);
   const hipStream_t st = as_stream(stream);
   const bool int8 = cache->format == KVP_CACHE_INT8;
   const dim3 grid(static_cast<unsigned>(p.cells * p.chunks));
+  const bool keep = p.logit_bytes != 0;
   if (int8)
-    cache_attend_kernel<KVP_CACHE_INT8><<<grid, kThreads, 0, st>>>(a);
+    (keep ? cache_attend_kernel<KVP_CACHE_INT8, true> : cache_attend_kernel<KVP_CACHE_INT8, false>)<<<grid, kThreads, 0, st>>>(a);
   else
-    cache_attend_kernel<KVP_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
-  if (p.chunks > 1) cache_join_kernel<<<dim3(static_cast<unsigned>(p.cells)), kThreads, 0, st>>>(a);
-  if (acc_out) {
+    (keep ? cache_attend_kernel<KVP_CACHE_E4M3, true> : cache_attend_kernel<KVP_CACHE_E4M3, false>)<<<grid, kThreads, 0, st>>>(a);
+  const uint32_t join_rows = std::min<uint32_t>(a.M, kTileRows), slices = static_cast<uint32_t>(ceil_div(max_len, kSlice));
+  const int64_t n_join = p.chunks > 1 ? p.cells * join_rows : 0, n_sum = p.logit_bytes ? p.cells * slices : 0;
+  if (n_join + n_sum > 0)
+    cache_join_kernel<<<dim3(static_cast<unsigned>(n_join + n_sum)), kThreads, 0, st>>>(a, static_cast<uint32_t>(n_join), join_rows, FastDiv(join_rows),
+                                                                                       slices, FastDiv(slices));
+  if (acc_out && !p.logit_bytes) {
     const int64_t groups = ceil_div(max_len, kTileTokens * kWaves), blocks = groups * cache->B * cache->H;
     const FastDiv div(static_cast<uint32_t>(groups));
     if (int8)

@@ -26,10 +26,12 @@ __device__ __forceinline__ uint32_t cache_len(const CacheArgs& c, uint32_t b) {
   const int32_t n = c.lens[b];
   return n < 0 ? 0u : min(static_cast<uint32_t>(n), c.max_blocks << c.bs_log2);
 }
+__device__ __forceinline__ uint32_t clamp_page(const CacheArgs& c, int32_t entry) {
+  return entry < 0 ? 0u : min(static_cast<uint32_t>(entry), c.num_blocks - 1);
+}
 // page index below max_blocks -> pool page
 __device__ __forceinline__ uint32_t cache_page(const CacheArgs& c, uint32_t b, uint32_t page) {
-  const int32_t p = c.table[static_cast<int64_t>(b) * c.table_stride + page];
-  return p < 0 ? 0u : min(static_cast<uint32_t>(p), c.num_blocks - 1);
+  return clamp_page(c, c.table[static_cast<int64_t>(b) * c.table_stride + page]);
 }
 
 // Validation of the fields that every call uses.

@@ -11,15 +11,15 @@
 // halves hold them).  Logits are kept in base 2.  The reference that exponentials are taken against follows the maximum
 // lazily: it moves only when a logit exceeds it by 2^8, which P in halves and the sums in fp32 bear.
 //
-// A block's waves take every fourth 64-token tile of its chunk; partial results of chunks are joined by a second kernel.
-// The weights of the tokens need the final statistics of their rows, so a further kernel forms the logits again.
+// This file: up to 16 query rows per (sequence, head), a decode step, bound by HBM.  A block's waves take a quarter of its chunk each; partial
+// results of chunks are joined by a second kernel.  The weights of the tokens need the final statistics of their rows: the logits are
+// kept and the second kernel sums them.  More rows: cache_attend_rows.hip.
 
 #include <math.h>
 
 #include <type_traits>
 
-#include "cache_attend_plan.h"
-#include "cache_common.h"
+#include "cache_attend.h"
 
 namespace kvp {
 namespace {
@@ -28,65 +28,9 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = kAttendWaves;
 constexpr int kThreads = kWaves * kWave;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.0f;              // how far (base 2) a logit may exceed the reference of its row
-constexpr float kValueSlack = 64.0f;        // and a page's value scale the reference scale: 2^8 * 2^6 fits a half
-constexpr float kLeastScale = 0x1p-100f;    // value scales below this count as this one's fractions
-constexpr float kLeast = -3.402823466e38f;
 constexpr int kKeptFloats = 4096;           // logits that a wave keeps in LDS: 4 tiles of 16 rows, 8 of 8
 constexpr int kOutPitch = 132;              // floats per row of partial outputs in LDS
 constexpr uint32_t kSlice = 4 * kThreads;   // tokens of a block that sums weights from logits
-
-struct AttendArgs {
-  CacheArgs c;
-  const uint16_t* q;
-  uint16_t* out;
-  int64_t q_sb, q_sw, q_sh, o_sb, o_sw, o_sh;
-  const int32_t* q_lens;
-  uint32_t W, G, M, row_tiles, max_len, chunk, chunks;
-  FastDiv div_tiles, div_h, div_g, div_chunks;
-  float scale2;                             // scale * log2(e)
-  int32_t causal;
-  float* part_out;                          // [cell][chunk][16][128] unnormalized, or null (one chunk)
-  float2* part_stat;                        // [cell][chunk][16] (reference, sum)
-  float2* row_stat;                         // [cell][16] (reference, 1 / sum): weights of more than one row tile
-  float* logits;                            // [cell][tile of 64 tokens][i][M][g][4], see the kernel: weights of a single row tile
-  int64_t logit_stride;
-  const float* acc_in;
-  float* acc_out;
-  int64_t acc_stride;
-};
-
-// What a row tile of a (sequence, head) sees.
-struct Rows {
-  uint32_t b, h, tile, n;                   // n: tokens of the sequence
-  int32_t m;                                // query tokens of the sequence
-  uint32_t least, most;                     // tokens seen by the tile's first and last row (most: by any)
-};
-
-__device__ __forceinline__ uint32_t seen_by(const AttendArgs& a, uint32_t n, int32_t m, uint32_t w) {
-  if (!a.causal) return n;
-  const int64_t p = static_cast<int64_t>(n) - m + w + 1;
-  return p < 0 ? 0u : static_cast<uint32_t>(p);   // w < m: at most n
-}
-
-__device__ __forceinline__ Rows rows_of(const AttendArgs& a, uint32_t cell) {
-  Rows r;
-  const uint32_t bh = a.div_tiles.quot(cell);
-  r.tile = cell - bh * a.row_tiles;
-  r.b = a.div_h.quot(bh);
-  r.h = bh - r.b * a.c.H;
-  r.n = min(cache_len(a.c, r.b), a.max_len);
-  r.m = static_cast<int32_t>(a.W);
-  if (a.q_lens) r.m = min(max(a.q_lens[r.b], 0), r.m);
-  const uint32_t w0 = a.div_g.quot(r.tile * kTileRows), w1 = a.div_g.quot(min(r.tile * kTileRows + kTileRows, a.M) - 1);
-  r.least = r.most = 0;
-  if (static_cast<int32_t>(w0) < r.m) {
-    r.least = seen_by(a, r.n, r.m, w0);
-    r.most = seen_by(a, r.n, r.m, min(w1, static_cast<uint32_t>(r.m) - 1));
-  }
-  return r;
-}
 
 // One query row as operands of the four channel steps: halves of q / 2^e with the sign of the softmax scale, and the positive factor that turns
 // their products with codes into base-2 logits.
@@ -113,17 +57,6 @@ __device__ __forceinline__ float load_query(const uint16_t* row, int g, bool val
 #pragma unroll
     for (int i = 0; i < 8; ++i) qf[s][i] = static_cast<_Float16>(ldexpf(x[s][i] * sign, -e));
   return ldexpf(fabsf(scale2), e);
-}
-
-// Table entry of the 16-token run that starts at token t, and the pool cell that it names; runs behind the last token take its page.
-__device__ __forceinline__ int32_t run_entry(const AttendArgs& a, uint32_t b, uint32_t t, uint32_t n) {
-  return a.c.table[static_cast<int64_t>(b) * a.c.table_stride + (min(t, n - 1) >> a.c.bs_log2)];
-}
-__device__ __forceinline__ int64_t entry_cell(const AttendArgs& a, uint32_t h, int32_t entry) {
-  return static_cast<int64_t>(clamp_page(a.c, entry)) * a.c.H + h;
-}
-__device__ __forceinline__ int64_t run_cell(const AttendArgs& a, uint32_t b, uint32_t h, uint32_t t, uint32_t n) {
-  return entry_cell(a, h, run_entry(a, b, t, n));
 }
 
 __device__ __forceinline__ uint32_t run_k_of(uint32_t t, int col) { return t + 16 * (col >> 2); }
@@ -330,18 +263,18 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
   const uint32_t r_out = r.tile * kTileRows + orow, w_out = a.div_g.quot(r_out);
   if (r_out >= a.M || static_cast<int32_t>(w_out) >= r.m) return;
   const float inv = z > 0.0f ? 1.0f / z : 0.0f;
-  if (a.row_stat && ch == 0) a.row_stat[static_cast<int64_t>(cell) * kTileRows + orow] = make_float2(m, inv);
+  if (a.row_bias && ch == 0) a.row_bias[static_cast<int64_t>(cell) * kTileRows + orow] = bias_of(m, z);
   uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w_out) * a.o_sw +
                   static_cast<int64_t>(r.h * a.G + (r_out - w_out * a.G)) * a.o_sh + ch;
   *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv),
                                               pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
 }
 
-// Row statistics over the chunks of a cell, by the 16 lanes that share `row`: (reference, 1 / sum); n chunks.
-__device__ __forceinline__ float2 joined_stats(const float2* st, uint32_t n, uint32_t lane16) {
+// Row statistics over the chunks of a cell, by the 16 lanes that share `row`: (reference, sum); n chunks, `pitch` rows apart.
+__device__ __forceinline__ float2 joined_stats(const float2* st, uint32_t pitch, uint32_t n, uint32_t lane16) {
   float m = kLeast, z = 0.0f;
   for (uint32_t i = lane16; i < n; i += 16) {
-    const float2 s = st[static_cast<int64_t>(i) * kTileRows];
+    const float2 s = st[static_cast<int64_t>(i) * pitch];
     const float m_new = fmaxf(m, s.x);
     z = fmaf(z, __builtin_amdgcn_exp2f(m - m_new), s.y * __builtin_amdgcn_exp2f(s.x - m_new));
     m = m_new;
@@ -354,7 +287,7 @@ __device__ __forceinline__ float2 joined_stats(const float2* st, uint32_t n, uin
     z = lo + hi;
     m = m_new;
   }
-  return make_float2(m, z > 0.0f ? 1.0f / z : 0.0f);
+  return make_float2(m, z);
 }
 
 // The chunks of a row joined (blocks below n_join: one per row of a cell), and, with logits kept, what every token drew
@@ -367,19 +300,20 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
   if (blockIdx.x < n_join) {
     const uint32_t cell = div_rows.quot(blockIdx.x), orow = blockIdx.x - cell * join_rows;
     const Rows r = rows_of(a, cell);
-    const uint32_t row = r.tile * kTileRows + orow, w = a.div_g.quot(row);
+    const uint32_t row = r.tile * a.tile_rows + orow, w = a.div_g.quot(row);
     if (row >= a.M || static_cast<int32_t>(w) >= r.m) return;
     const uint32_t n = (r.most + a.chunk - 1) / a.chunk;
-    const float2* st = a.part_stat + static_cast<int64_t>(cell) * a.chunks * kTileRows + orow;
-    const float2 stat = joined_stats(st, n, tid & 15);
-    if (a.row_stat && tid == 0) a.row_stat[static_cast<int64_t>(cell) * kTileRows + orow] = stat;
+    const float2* st = a.part_stat + static_cast<int64_t>(cell) * a.chunks * a.tile_rows + orow;
+    const float2 stat = joined_stats(st, a.tile_rows, n, tid & 15);
+    if (a.row_bias && tid == 0) a.row_bias[static_cast<int64_t>(cell) * a.tile_rows + orow] = bias_of(stat.x, stat.y);
+    const float inv = stat.y > 0.0f ? 1.0f / stat.y : 0.0f;
     const uint32_t group = tid >> 5, ch = tid & 31;
-    const float4* po = reinterpret_cast<const float4*>(a.part_out + (static_cast<int64_t>(cell) * a.chunks * kTileRows + orow) * kHeadDim) + ch;
+    const float4* po = reinterpret_cast<const float4*>(a.part_out + (static_cast<int64_t>(cell) * a.chunks * a.tile_rows + orow) * kHeadDim) + ch;
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
     for (uint32_t i = group; i < n; i += 8) {
-      const float f = __builtin_amdgcn_exp2f(st[static_cast<int64_t>(i) * kTileRows].x - stat.x);
-      const float4 u = po[static_cast<int64_t>(i) * (kTileRows * kHeadDim / 4)];
+      const float f = __builtin_amdgcn_exp2f(st[static_cast<int64_t>(i) * a.tile_rows].x - stat.x);
+      const float4 u = po[static_cast<int64_t>(i) * a.tile_rows * (kHeadDim / 4)];
       y.x = fmaf(u.x, f, y.x); y.y = fmaf(u.y, f, y.y); y.z = fmaf(u.z, f, y.z); y.w = fmaf(u.w, f, y.w);
     }
     part_s[group][ch] = y;
@@ -392,7 +326,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
     }
     uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw +
                     static_cast<int64_t>(r.h * a.G + (row - w * a.G)) * a.o_sh + ch * 4;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(y.x * stat.y, y.y * stat.y), pack_bf16x2(y.z * stat.y, y.w * stat.y));
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
     return;
   }
   // one row tile per (sequence, head) here: a cell is a (sequence, head)
@@ -403,8 +337,8 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
     const uint32_t orow = tid >> 4, w = a.div_g.quot(orow);
     float2 stat = make_float2(0.0f, 0.0f);
     if (orow < a.M && static_cast<int32_t>(w) < r.m)
-      stat = joined_stats(a.part_stat + static_cast<int64_t>(cell) * a.chunks * kTileRows + orow, (r.most + a.chunk - 1) / a.chunk, tid & 15);
-    if ((tid & 15) == 0) stat_s[orow] = stat;
+      stat = joined_stats(a.part_stat + static_cast<int64_t>(cell) * a.chunks * a.tile_rows + orow, a.tile_rows, (r.most + a.chunk - 1) / a.chunk, tid & 15);
+    if ((tid & 15) == 0) stat_s[orow] = make_float2(stat.x, stat.y > 0.0f ? 1.0f / stat.y : 0.0f);
   }
   __syncthreads();
   // 16 threads a tile, thread 4 i + g has tokens 16 g + 4 i ..+3
@@ -426,48 +360,6 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i)
     if (t + i < r.n) a.acc_out[at + i] = (a.acc_in ? a.acc_in[at + i] : 0.0f) + drawn[i];
-}
-
-// What every token drew: a wave owns 64 tokens of a (sequence, head) and goes through all query rows that see them; its sums
-// are complete and formed in one order.
-template <int FMT>
-__global__ __launch_bounds__(kThreads) void cache_weights_kernel(const AttendArgs a, uint32_t groups, FastDiv div_groups) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-  const uint32_t bh = div_groups.quot(blockIdx.x), t = ((blockIdx.x - bh * groups) * kWaves + wave) * kTileTokens;
-  const uint32_t b = a.div_h.quot(bh), h = bh - b * a.c.H;
-  const uint32_t n = min(cache_len(a.c, b), a.max_len);
-  if (t >= n) return;
-  const uint32_t run_k = t + 16 * (col >> 2), run = t + 16 * g;
-  uint4 k[4][2];
-  load_keys(a, run_cell(a, b, h, run_k, n), run_k, lane, k);
-  const float ks = a.c.k_scales[run_cell(a, b, h, run, n)];
-  float drawn[16] = {};
-  for (uint32_t tile = 0; tile < a.row_tiles; ++tile) {
-    const Rows r = rows_of(a, bh * a.row_tiles + tile);
-    if (r.most <= t) continue;               // uniform
-    const uint32_t row = tile * kTileRows + col, w = a.div_g.quot(row), head = h * a.G + (row - w * a.G);
-    const bool valid = row < a.M && static_cast<int32_t>(w) < r.m;
-    half8_t qf[4];
-    const float qs = load_query(a.q + static_cast<int64_t>(b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh, g,
-                                valid, a.scale2, qf);
-    const uint32_t limit = valid ? seen_by(a, n, r.m, w) : 0u;
-    const float2 st = valid ? a.row_stat[(static_cast<int64_t>(bh) * a.row_tiles + tile) * kTileRows + col] : make_float2(0.0f, 0.0f);
-    floatx4 s[4];
-    logits<FMT>(k, qf, s);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float p = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] * (ks * qs) - st.x) * st.y;
-      drawn[i] += run + i < limit ? p : 0.0f;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) drawn[i] += __shfl_xor(drawn[i], d);
-  const int64_t at = static_cast<int64_t>(bh) * a.acc_stride + run;
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (col == i && run + i < n) a.acc_out[at + i] = (a.acc_in ? a.acc_in[at + i] : 0.0f) + drawn[i];
 }
 
 }  // namespace
@@ -494,7 +386,7 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   if (acc_out && acc_stride < max_len) return KVP_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(q_lens) | reinterpret_cast<uintptr_t>(acc_in) | reinterpret_cast<uintptr_t>(acc_out)) & 3u) return KVP_ERR_ALIGN;
   const AttendPlan p = make_attend_plan(cache->B, cache->H, q->H, W, max_len, acc_out != nullptr);
-  if (p.cells * std::max<int64_t>(p.chunks, kTileRows) + p.cells * ceil_div(max_len, kSlice) >= (1ll << 31)) return KVP_ERR_SHAPE;
+  if (p.cells * std::max(p.chunks, p.tile_rows) + p.cells * ceil_div(max_len, kSlice) >= (1ll << 31)) return KVP_ERR_SHAPE;
   if (p.bytes != 0 && (!ws || ws_bytes < p.bytes || !aligned16(ws))) return KVP_ERR_WORKSPACE;
   AttendArgs a{};
   a.c = cache_args(cache);
@@ -506,6 +398,7 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   a.W = static_cast<uint32_t>(W);
   a.G = static_cast<uint32_t>(G);
   a.M = a.W * a.G;
+  a.tile_rows = static_cast<uint32_t>(p.tile_rows);
   a.row_tiles = static_cast<uint32_t>(p.row_tiles);
   a.max_len = static_cast<uint32_t>(max_len);
   a.chunk = static_cast<uint32_t>(p.chunk);
@@ -519,7 +412,7 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   char* w = static_cast<char*>(ws);
   if (p.out_bytes) a.part_out = reinterpret_cast<float*>(w);
   if (p.stat_bytes) a.part_stat = reinterpret_cast<float2*>(w + p.out_bytes);
-  if (p.row_bytes) a.row_stat = reinterpret_cast<float2*>(w + p.out_bytes + p.stat_bytes);
+  if (p.row_bytes) a.row_bias = reinterpret_cast<float*>(w + p.out_bytes + p.stat_bytes);
   if (p.logit_bytes) a.logits = reinterpret_cast<float*>(w + p.out_bytes + p.stat_bytes + p.row_bytes);
   a.logit_stride = p.logit_stride;
   a.acc_in = acc_in;
@@ -529,22 +422,17 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   const bool int8 = cache->format == KVP_CACHE_INT8;
   const dim3 grid(static_cast<unsigned>(p.cells * p.chunks));
   const bool keep = p.logit_bytes != 0;
-  if (int8)
+  if (p.tile_rows > kTileRows)
+    attend_rows_launch(a, p.cells * p.chunks, cache->format, st);
+  else if (int8)
     (keep ? cache_attend_kernel<KVP_CACHE_INT8, true> : cache_attend_kernel<KVP_CACHE_INT8, false>)<<<grid, kThreads, 0, st>>>(a);
   else
     (keep ? cache_attend_kernel<KVP_CACHE_E4M3, true> : cache_attend_kernel<KVP_CACHE_E4M3, false>)<<<grid, kThreads, 0, st>>>(a);
-  const uint32_t join_rows = std::min<uint32_t>(a.M, kTileRows), slices = static_cast<uint32_t>(ceil_div(max_len, kSlice));
+  const uint32_t join_rows = std::min(a.M, a.tile_rows), slices = static_cast<uint32_t>(ceil_div(max_len, kSlice));
   const int64_t n_join = p.chunks > 1 ? p.cells * join_rows : 0, n_sum = p.logit_bytes ? p.cells * slices : 0;
   if (n_join + n_sum > 0)
     cache_join_kernel<<<dim3(static_cast<unsigned>(n_join + n_sum)), kThreads, 0, st>>>(a, static_cast<uint32_t>(n_join), join_rows, FastDiv(join_rows),
                                                                                        slices, FastDiv(slices));
-  if (acc_out && !p.logit_bytes) {
-    const int64_t groups = ceil_div(max_len, kTileTokens * kWaves), blocks = groups * cache->B * cache->H;
-    const FastDiv div(static_cast<uint32_t>(groups));
-    if (int8)
-      cache_weights_kernel<KVP_CACHE_INT8><<<dim3(static_cast<unsigned>(blocks)), kThreads, 0, st>>>(a, static_cast<uint32_t>(groups), div);
-    else
-      cache_weights_kernel<KVP_CACHE_E4M3><<<dim3(static_cast<unsigned>(blocks)), kThreads, 0, st>>>(a, static_cast<uint32_t>(groups), div);
-  }
+  if (acc_out && !p.logit_bytes) weights_rows_launch(a, cache->format, st);
   return launch_status();
 }

@@ -1,7 +1,7 @@
 // kvp_cache_append and kvp_cache_read: bf16 K/V rows into the 8-bit paged cache and back.
 //
-// Append: a block owns one page of one head, keys or values: it reads the page's new rows (kept in registers), reduces
-// their largest magnitude, settles the page's scale, recodes what the page held where that scale grew, and stores the codes.
+// Append: a block owns one page of one head, keys and values: it reads the page's new rows (kept in registers), reduces
+// their largest magnitudes, settles the page's scales, recodes what the page held where a scale grew, and stores the codes.
 // Values are stored channel-major: a row's codes are turned in LDS, and whole runs of 16 slots of a channel go out as 16 bytes.
 // Read: the same blocks the other way.
 // Both move 2 + 1 bytes per element and are bound by HBM; a decode step (one row per sequence) is bound by latency.
@@ -12,7 +12,6 @@ namespace kvp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxItems = 8;      // 16-byte pieces of a page's rows per thread: bs / 16
 
 struct AppendArgs {
   CacheArgs c;
@@ -55,15 +54,115 @@ __device__ __forceinline__ uint32_t recode4(uint32_t w, float old, const PageQua
   return q.codes4<FMT>(x);
 }
 
-template <int FMT>
+// What a page of a plane becomes: scale before and after, and whether its older codes are coded again.
+struct PageScale {
+  float old, scale;
+  bool recode;
+};
+
+// Slot of a thread's item: consecutive ones, so that the codes of up to four slots of a channel leave as a word.
+template <int ITEMS>
+__device__ __forceinline__ int slot_of(int i) { return static_cast<int>(threadIdx.x >> 4) * ITEMS + i; }
+
+// Bytes of four words turned: out[k] = bytes k of w[0 .. 3]
+__device__ __forceinline__ void turn4(const uint32_t w[4], uint32_t out[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+  const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  out[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+  out[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  out[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+  out[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
+// Keys of a page: new rows' codes, older ones again where the scale grew.
+template <int FMT, int ITEMS>
+__device__ __forceinline__ void store_keys(const uint4 (&raw)[ITEMS], const PageScale& ps, uint8_t* codes, int s0, int s1) {
+  const PageQuantizer q(ps.scale);
+  const int ch = static_cast<int>(threadIdx.x & 15) * 8;
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const int slot = slot_of<ITEMS>(i);
+    uint2* at = reinterpret_cast<uint2*>(codes + slot * kHeadDim + ch);
+    if (slot >= s0 && slot < s1) {
+      float x[8];
+      unpack_bf16x8(raw[i], x);
+      *at = make_uint2(q.codes4<FMT>(x), q.codes4<FMT>(x + 4));
+    } else if (ps.recode && slot < s0) {
+      const uint2 v = *at;
+      *at = make_uint2(recode4<FMT>(v.x, ps.old, q), recode4<FMT>(v.y, ps.old, q));
+    }
+  }
+}
+
+// Values of a page, turned in LDS: [channel][slot], 4 bytes more than a page's slots apart.
+template <int FMT, int ITEMS>
+__device__ __forceinline__ void store_values(const uint4 (&raw)[ITEMS], const PageScale& ps, uint8_t* codes, int s0, int s1, uint8_t* turn) {
+  constexpr int bs = 16 * ITEMS, pitch = bs + 4;
+  const PageQuantizer q(ps.scale);
+  const int ch = static_cast<int>(threadIdx.x & 15) * 8;
+  uint32_t w[ITEMS][2];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {   // rows that are not new are zeros, and their codes are not used
+    float x[8];
+    unpack_bf16x8(raw[i], x);
+    w[i][0] = q.codes4<FMT>(x);
+    w[i][1] = q.codes4<FMT>(x + 4);
+  }
+  uint8_t* to = turn + ch * pitch + slot_of<ITEMS>(0);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if constexpr (ITEMS == 1)
+      to[k * pitch] = static_cast<uint8_t>(w[0][k >> 2] >> (8 * (k & 3)));
+    else if constexpr (ITEMS == 2)
+      *reinterpret_cast<uint16_t*>(to + k * pitch) =
+          static_cast<uint16_t>(((w[0][k >> 2] >> (8 * (k & 3))) & 0xffu) | (((w[1][k >> 2] >> (8 * (k & 3))) & 0xffu) << 8));
+  }
+  if constexpr (ITEMS >= 4) {
+#pragma unroll
+    for (int g = 0; g < ITEMS; g += 4)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t in[4] = {w[g][j], w[g + 1][j], w[g + 2][j], w[g + 3][j]};
+        uint32_t out[4];
+        turn4(in, out);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<uint32_t*>(to + (4 * j + k) * pitch + g) = out[k];
+      }
+  }
+  __syncthreads();
+  // every run of 16 slots of a channel that changes
+#pragma unroll
+  for (int i = 0; i < (ITEMS + 1) / 2; ++i) {
+    const int n = static_cast<int>(threadIdx.x) + i * kThreads, c = n / ITEMS, run = n % ITEMS, lo = s0 - run * 16, hi = s1 - run * 16;   // new bytes of the run
+    if (n >= kHeadDim * ITEMS) break;
+    const bool changes = hi > 0 && lo < 16;
+    if (!changes && !(ps.recode && lo > 0)) continue;
+    uint4* at = reinterpret_cast<uint4*>(codes + c * bs + run * 16);
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(turn + c * pitch + run * 16);
+    const uint4 fresh16 = make_uint4(from[0], from[1], from[2], from[3]);
+    if (lo <= 0 && hi >= 16) {
+      *at = fresh16;
+      continue;
+    }
+    uint4 v = *at;
+    if (ps.recode && lo > 0) {
+      const uint4 again = make_uint4(recode4<FMT>(v.x, ps.old, q), recode4<FMT>(v.y, ps.old, q), recode4<FMT>(v.z, ps.old, q), recode4<FMT>(v.w, ps.old, q));
+      v = blend(byte_mask(0, lo), again, v);
+    }
+    *at = changes ? blend(byte_mask(lo, hi), fresh16, v) : v;
+  }
+}
+
+// ITEMS: 16-byte pieces of a page's rows per thread and plane, bs / 16
+template <int FMT, int ITEMS>
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (128 + 16)];   // values: [channel][slot], pitch bs + 16
-  __shared__ float max_s[4];
+  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (16 * ITEMS + 4)];
+  __shared__ float max_s[2][4];
   const CacheArgs& c = a.c;
-  // block -> (sequence, plane, page of the call, head)
-  const uint32_t rest = a.div_h.quot(blockIdx.x), h = blockIdx.x - rest * c.H;
-  const uint32_t bp = a.div_pages.quot(rest), p = rest - bp * a.pages, b = bp >> 1, plane = bp & 1;
-  const uint32_t bs = 1u << c.bs_log2, len = cache_len(c, b);
+  // block -> (sequence, page of the call, head)
+  const uint32_t bp = a.div_h.quot(blockIdx.x), h = blockIdx.x - bp * c.H, b = a.div_pages.quot(bp), p = bp - b * a.pages;
+  constexpr uint32_t bs = 16 * ITEMS;
+  const uint32_t len = cache_len(c, b);
   uint32_t count = a.W;
   if (a.counts) count = static_cast<uint32_t>(min(max(a.counts[b], 0), static_cast<int32_t>(a.W)));
   const uint32_t end = min(len + count, c.max_blocks << c.bs_log2);
@@ -71,94 +170,64 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(const AppendArgs
   if (max(t0, len) >= end) return;
   const int s0 = static_cast<int>(max(len, t0) - t0), s1 = static_cast<int>(min(end - t0, bs));   // new slots
   const int64_t cell = static_cast<int64_t>(cache_page(c, b, page)) * c.H + h;
-  const uint16_t* src = a.src[plane] + static_cast<int64_t>(b) * a.sb[plane] + static_cast<int64_t>(h) * a.sh[plane];
-  const int64_t sw = a.sw[plane];
   const int64_t w0 = static_cast<int64_t>(t0) - len;                        // row of slot 0
-  const int items = static_cast<int>(bs >> 4);
 
-  uint4 raw[kMaxItems];
-  float amax = 0.0f;
+  uint4 raw[2][ITEMS];
 #pragma unroll
-  for (int i = 0; i < kMaxItems; ++i) {
-    if (i >= items) break;
-    const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4);
-    raw[i] = make_uint4(0, 0, 0, 0);
-    if (slot >= s0 && slot < s1) raw[i] = load_stream16(src + (w0 + slot) * sw + (threadIdx.x & 15) * 8);
+  for (int plane = 0; plane < 2; ++plane) {
+    const uint16_t* src = a.src[plane] + static_cast<int64_t>(b) * a.sb[plane] + static_cast<int64_t>(h) * a.sh[plane] + (threadIdx.x & 15) * 8;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int slot = slot_of<ITEMS>(i);
+      raw[plane][i] = make_uint4(0, 0, 0, 0);
+      if (slot >= s0 && slot < s1) raw[plane][i] = load_stream16(src + (w0 + slot) * a.sw[plane]);
+    }
   }
-  float* scale_at = (plane ? c.v_scales : c.k_scales) + cell;
-  const float old = s0 > 0 ? *scale_at : 0.0f;
+  PageScale ps[2];
+  ps[0].old = s0 > 0 ? c.k_scales[cell] : 0.0f;
+  ps[1].old = s0 > 0 ? c.v_scales[cell] : 0.0f;
+  float amax[2];
 #pragma unroll
-  for (int i = 0; i < kMaxItems; ++i) {
-    if (i >= items) break;
-    float x[8];
-    unpack_bf16x8(raw[i], x);
-    amax = fmaxf(amax, abs_max8(x));
-  }
-  amax = block_max256(amax, max_s);
-  const float fresh = amax / kCodeMax<FMT>, scale = s0 > 0 ? fmaxf(old, fresh) : fresh;
-  const bool recode = s0 > 0 && scale != old;
-  const PageQuantizer q(scale);
-  if (threadIdx.x == 0 && (s0 == 0 || recode)) *scale_at = scale;
-
-  uint8_t* codes = (plane ? c.v_codes : c.k_codes) + (cell << (c.bs_log2 + 7));
-  const int pitch = static_cast<int>(bs) + 16;
+  for (int plane = 0; plane < 2; ++plane) {
+    amax[plane] = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kMaxItems; ++i) {
-    if (i >= items) break;
-    const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4), ch = static_cast<int>(threadIdx.x & 15) * 8;
-    const bool is_new = slot >= s0 && slot < s1;
-    uint2 w;
-    if (is_new) {
+    for (int i = 0; i < ITEMS; ++i) {
       float x[8];
-      unpack_bf16x8(raw[i], x);
-      w = make_uint2(q.codes4<FMT>(x), q.codes4<FMT>(x + 4));
+      unpack_bf16x8(raw[plane][i], x);
+      amax[plane] = fmaxf(amax[plane], abs_max8(x));
     }
-    if (plane == 0) {
-      uint2* at = reinterpret_cast<uint2*>(codes + slot * kHeadDim + ch);
-      if (is_new) {
-        *at = w;
-      } else if (recode && slot < s0) {
-        const uint2 v = *at;
-        *at = make_uint2(recode4<FMT>(v.x, old, q), recode4<FMT>(v.y, old, q));
-      }
-    } else if (is_new) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        turn_s[(ch + k) * pitch + slot] = static_cast<uint8_t>(w.x >> (8 * k));
-        turn_s[(ch + 4 + k) * pitch + slot] = static_cast<uint8_t>(w.y >> (8 * k));
-      }
-    }
+    amax[plane] = wave_max(amax[plane]);
+    if ((threadIdx.x & 63) == 0) max_s[plane][threadIdx.x >> 6] = amax[plane];
   }
-  if (plane == 0) return;
   __syncthreads();
-  // values: every run of 16 slots of a channel that changes
-  for (int i = static_cast<int>(threadIdx.x); i < kHeadDim * items; i += kThreads) {
-    const int ch = i >> (c.bs_log2 - 4), run = i & (items - 1), lo = s0 - run * 16, hi = s1 - run * 16;   // new bytes of the run
-    const bool changes = hi > 0 && lo < 16;
-    if (!changes && !(recode && lo > 0)) continue;
-    uint4* at = reinterpret_cast<uint4*>(codes + (ch << c.bs_log2) + run * 16);
-    const uint4 fresh16 = *reinterpret_cast<const uint4*>(turn_s + ch * pitch + run * 16);
-    if (lo <= 0 && hi >= 16) {
-      *at = fresh16;
-      continue;
-    }
-    uint4 v = *at;
-    if (recode && lo > 0) {
-      const uint4 again = make_uint4(recode4<FMT>(v.x, old, q), recode4<FMT>(v.y, old, q), recode4<FMT>(v.z, old, q), recode4<FMT>(v.w, old, q));
-      v = blend(byte_mask(0, lo), again, v);
-    }
-    *at = changes ? blend(byte_mask(lo, hi), fresh16, v) : v;
+#pragma unroll
+  for (int plane = 0; plane < 2; ++plane) {
+    const float fresh = fmaxf(fmaxf(max_s[plane][0], max_s[plane][1]), fmaxf(max_s[plane][2], max_s[plane][3])) / kCodeMax<FMT>;
+    ps[plane].scale = s0 > 0 ? fmaxf(ps[plane].old, fresh) : fresh;
+    ps[plane].recode = s0 > 0 && ps[plane].scale != ps[plane].old;
+    if (threadIdx.x == 0 && (s0 == 0 || ps[plane].recode)) (plane ? c.v_scales : c.k_scales)[cell] = ps[plane].scale;
   }
+  store_keys<FMT>(raw[0], ps[0], c.k_codes + (cell << (c.bs_log2 + 7)), s0, s1);
+  store_values<FMT>(raw[1], ps[1], c.v_codes + (cell << (c.bs_log2 + 7)), s0, s1, turn_s);
 }
 
+// Eight codes on a scale as bf16 (one product and one rounding each)
 template <int FMT>
+__device__ __forceinline__ uint4 restore8(uint32_t w0, uint32_t w1, float scale) {
+  float x[8];
+  decode4<FMT>(w0, x);
+  decode4<FMT>(w1, x + 4);
+  return make_uint4(pack_bf16x2(x[0] * scale, x[1] * scale), pack_bf16x2(x[2] * scale, x[3] * scale), pack_bf16x2(x[4] * scale, x[5] * scale),
+                    pack_bf16x2(x[6] * scale, x[7] * scale));
+}
+
+template <int FMT, int ITEMS>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (128 + 16)];
+  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (16 * ITEMS + 16)];
   const CacheArgs& c = a.c;
-  const uint32_t rest = a.div_h.quot(blockIdx.x), h = blockIdx.x - rest * c.H;
-  const uint32_t bp = a.div_pages.quot(rest), p = rest - bp * a.pages, b = bp >> 1, plane = bp & 1;
-  if (!a.dst[plane]) return;
-  const uint32_t bs = 1u << c.bs_log2;
+  const uint32_t bp = a.div_h.quot(blockIdx.x), h = blockIdx.x - bp * c.H, b = a.div_pages.quot(bp), p = bp - b * a.pages;
+  constexpr uint32_t bs = 16 * ITEMS;
+  constexpr int pitch = 16 * ITEMS + 16;
   const uint32_t first = a.first ? static_cast<uint32_t>(max(a.first[b], 0)) : 0u;
   const uint32_t end = min(cache_len(c, b), first + a.R), page = (first >> c.bs_log2) + p;
   if (page >= c.max_blocks) return;
@@ -166,44 +235,66 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a) 
   if (max(t0, first) >= end) return;
   const int s0 = static_cast<int>(max(first, t0) - t0), s1 = static_cast<int>(min(end - t0, bs));
   const int64_t cell = static_cast<int64_t>(cache_page(c, b, page)) * c.H + h;
-  const uint8_t* codes = (plane ? c.v_codes : c.k_codes) + (cell << (c.bs_log2 + 7));
-  const float scale = (plane ? c.v_scales : c.k_scales)[cell];
-  uint16_t* dst = a.dst[plane] + static_cast<int64_t>(b) * a.sb[plane] + static_cast<int64_t>(h) * a.sh[plane];
   const int64_t r0 = static_cast<int64_t>(t0) - first;                       // out row of slot 0
-  const int items = static_cast<int>(bs >> 4), pitch = static_cast<int>(bs) + 16;
-  if (plane) {
-    for (int i = static_cast<int>(threadIdx.x); i < kHeadDim * items; i += kThreads) {
-      const int ch = i >> (c.bs_log2 - 4), run = i & (items - 1);
-      *reinterpret_cast<uint4*>(turn_s + ch * pitch + run * 16) = load_stream16(codes + (ch << c.bs_log2) + run * 16);
+  const uint8_t* k_codes = c.k_codes + (cell << (c.bs_log2 + 7));
+  const uint8_t* v_codes = c.v_codes + (cell << (c.bs_log2 + 7));
+  uint2 k[ITEMS];
+  uint4 v[(ITEMS + 1) / 2];
+  if (a.dst[1]) {
+#pragma unroll
+    for (int i = 0; i < (ITEMS + 1) / 2; ++i)
+      if (threadIdx.x + i * kThreads < kHeadDim * ITEMS) v[i] = load_stream16(v_codes + (threadIdx.x + i * kThreads) * 16);   // the page as it lies
+  }
+  if (a.dst[0]) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) k[i] = load_stream8(k_codes + (threadIdx.x + i * kThreads) * 8);
+  }
+  const float k_scale = c.k_scales[cell], v_scale = c.v_scales[cell];
+  if (a.dst[1]) {
+#pragma unroll
+    for (int i = 0; i < (ITEMS + 1) / 2; ++i) {
+      const int n = static_cast<int>(threadIdx.x + i * kThreads), ch = n / ITEMS, run = n % ITEMS;
+      if (n < kHeadDim * ITEMS) *reinterpret_cast<uint4*>(turn_s + ch * pitch + run * 16) = v[i];
     }
     __syncthreads();
   }
 #pragma unroll
-  for (int i = 0; i < kMaxItems; ++i) {
-    if (i >= items) break;
+  for (int i = 0; i < ITEMS; ++i) {
     const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4), ch = static_cast<int>(threadIdx.x & 15) * 8;
     if (slot < s0 || slot >= s1) continue;
-    uint32_t w[2];
-    if (plane) {
+    if (a.dst[0])
+      store_stream16(a.dst[0] + static_cast<int64_t>(b) * a.sb[0] + static_cast<int64_t>(h) * a.sh[0] + (r0 + slot) * a.sr[0] + ch,
+                     restore8<FMT>(k[i].x, k[i].y, k_scale));
+    if (a.dst[1]) {
+      uint32_t w[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint8_t* at = turn_s + (ch + 4 * k) * pitch + slot;
-        w[k] = at[0] | (at[pitch] << 8) | (at[2 * pitch] << 16) | (static_cast<uint32_t>(at[3 * pitch]) << 24);
+      for (int j = 0; j < 2; ++j) {
+        const uint8_t* at = turn_s + (ch + 4 * j) * pitch + slot;
+        w[j] = at[0] | (at[pitch] << 8) | (at[2 * pitch] << 16) | (static_cast<uint32_t>(at[3 * pitch]) << 24);
       }
-    } else {
-      const uint2 v = load_stream8(codes + slot * kHeadDim + ch);
-      w[0] = v.x;
-      w[1] = v.y;
+      store_stream16(a.dst[1] + static_cast<int64_t>(b) * a.sb[1] + static_cast<int64_t>(h) * a.sh[1] + (r0 + slot) * a.sr[1] + ch,
+                     restore8<FMT>(w[0], w[1], v_scale));
     }
-    uint32_t o[4];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float x[4];
-      decode4<FMT>(w[k], x);
-      o[2 * k] = pack_bf16x2(x[0] * scale, x[1] * scale);
-      o[2 * k + 1] = pack_bf16x2(x[2] * scale, x[3] * scale);
-    }
-    store_stream16(dst + (r0 + slot) * a.sr[plane] + ch, make_uint4(o[0], o[1], o[2], o[3]));
+  }
+}
+
+template <int FMT>
+void append_launch(const AppendArgs& a, dim3 grid, hipStream_t st) {
+  switch (a.c.bs_log2) {
+    case 4: cache_append_kernel<FMT, 1><<<grid, kThreads, 0, st>>>(a); break;
+    case 5: cache_append_kernel<FMT, 2><<<grid, kThreads, 0, st>>>(a); break;
+    case 6: cache_append_kernel<FMT, 4><<<grid, kThreads, 0, st>>>(a); break;
+    default: cache_append_kernel<FMT, 8><<<grid, kThreads, 0, st>>>(a); break;
+  }
+}
+
+template <int FMT>
+void read_launch(const ReadArgs& a, dim3 grid, hipStream_t st) {
+  switch (a.c.bs_log2) {
+    case 4: cache_read_kernel<FMT, 1><<<grid, kThreads, 0, st>>>(a); break;
+    case 5: cache_read_kernel<FMT, 2><<<grid, kThreads, 0, st>>>(a); break;
+    case 6: cache_read_kernel<FMT, 4><<<grid, kThreads, 0, st>>>(a); break;
+    default: cache_read_kernel<FMT, 8><<<grid, kThreads, 0, st>>>(a); break;
   }
 }
 
@@ -229,16 +320,16 @@ extern "C" int32_t kvp_cache_append(const kvp_cache* cache, const kvp_view* k, c
   a.W = static_cast<uint32_t>(k->T);
   // W rows behind any number of older ones touch at most this many pages; never more than there are
   const int64_t pages = std::min<int64_t>(cache->max_blocks, ceil_div(k->T + cache->bs - 1, cache->bs));
-  const int64_t blocks = cache->B * cache->H * 2 * pages;
+  const int64_t blocks = cache->B * cache->H * pages;
   if (blocks >= (1ll << 31)) return KVP_ERR_SHAPE;
   a.pages = static_cast<uint32_t>(pages);
   a.div_h = FastDiv(a.c.H);
   a.div_pages = FastDiv(a.pages);
   const dim3 grid(static_cast<unsigned>(blocks));
   if (cache->format == KVP_CACHE_INT8)
-    cache_append_kernel<KVP_CACHE_INT8><<<grid, kThreads, 0, as_stream(stream)>>>(a);
+    append_launch<KVP_CACHE_INT8>(a, grid, as_stream(stream));
   else
-    cache_append_kernel<KVP_CACHE_E4M3><<<grid, kThreads, 0, as_stream(stream)>>>(a);
+    append_launch<KVP_CACHE_E4M3>(a, grid, as_stream(stream));
   return launch_status();
 }
 
@@ -264,15 +355,15 @@ extern "C" int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, 
   a.first = first;
   a.R = static_cast<uint32_t>(R);
   const int64_t pages = std::min<int64_t>(cache->max_blocks, ceil_div(R + cache->bs - 1, cache->bs));
-  const int64_t blocks = cache->B * cache->H * 2 * pages;
+  const int64_t blocks = cache->B * cache->H * pages;
   if (blocks >= (1ll << 31)) return KVP_ERR_SHAPE;
   a.pages = static_cast<uint32_t>(pages);
   a.div_h = FastDiv(a.c.H);
   a.div_pages = FastDiv(a.pages);
   const dim3 grid(static_cast<unsigned>(blocks));
   if (cache->format == KVP_CACHE_INT8)
-    cache_read_kernel<KVP_CACHE_INT8><<<grid, kThreads, 0, as_stream(stream)>>>(a);
+    read_launch<KVP_CACHE_INT8>(a, grid, as_stream(stream));
   else
-    cache_read_kernel<KVP_CACHE_E4M3><<<grid, kThreads, 0, as_stream(stream)>>>(a);
+    read_launch<KVP_CACHE_E4M3>(a, grid, as_stream(stream));
   return launch_status();
 }

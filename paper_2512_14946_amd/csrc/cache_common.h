@@ -137,15 +137,19 @@ struct PageQuantizer {
   }
 };
 
-// largest value over a 256-thread block of a non-negative number per thread; every thread gets it.  sh: 4 floats
-__device__ __forceinline__ float block_max256(float v, float* sh) {
+// largest value over the wave of a non-negative number per lane
+__device__ __forceinline__ float wave_max(float v) {
   uint32_t u = __float_as_uint(group_max(v, 16));
   u = max(u, static_cast<uint32_t>(__shfl_xor(static_cast<int>(u), 16)));
   u = max(u, static_cast<uint32_t>(__shfl_xor(static_cast<int>(u), 32)));
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = __uint_as_float(u);
+  return __uint_as_float(u);
+}
+// ... over a 256-thread block; every thread gets it.  sh: 4 floats
+__device__ __forceinline__ float block_max256(float v, float* sh) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  const float r = fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
-  return r;
+  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
 }
 
 }  // namespace kvp

@@ -1,13 +1,15 @@
 // kvp_rotary: rotary positions.  Every pair (a, b) of a row turns by t = position * freq[i]:
 //   y_a = m (a cos t - b sin t),  y_b = m (b cos t + a sin t)
 // The angle of a far position has too many bits for fp32 (131072 radians leave an error of 0.004), so position * freq / 2 pi and its
-// fraction are formed in double; the fraction of a turn in [-1/2, 1/2] loses nothing that matters in fp32.
+// fraction are formed in double; the fraction of a turn in [-1/2, 1/2] goes to v_sin_f32 / v_cos_f32, which take turns and are
+// off by at most 1.25e-7 there (all 2^24 multiples of 2^-24 compared with double; the results are rounded to bf16, 2^-9).
 //
-// Bound by HBM (x is read and written once) except where every head has positions of its own.  A block takes some
-// tokens with all their heads; one sine and cosine per (token, pair) go to LDS once and serve every head.  Lanes then
-// stream the rows: eight lanes share a row, each owns two 16-byte pieces, which hold both channels of its eight pairs
-// (half layout: pieces rotary_dim / 2 apart).  Pairs that do not fall on such pieces (half layout, rotary_dim not a multiple
-// of 16) take a kernel with two lanes' channels per element access.
+// Bound by HBM (x is read and written once): eight lanes share a row, each owns two 16-byte pieces, which hold both channels of
+// its eight pairs (half layout: pieces rotary_dim / 2 apart).  Where heads share a position a block takes some tokens with all
+// their heads, and one sine and cosine per (token, pair) go to LDS once and serve every head: 4 x 8192 x 8 rows 23.7 us, 5.7 TB/s.  With a position
+// per head a lane forms those of its own eight pairs: 80 x 4916 x 8 rows 273 us, 6.0 TB/s (580 us by way of
+// LDS with a library sincospi of 25 instructions).  Pairs that do not fall on such pieces (half layout, rotary_dim not a multiple of 16) take a
+// kernel with a wave per row.
 
 #include <math.h>
 
@@ -17,7 +19,8 @@ namespace kvp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 64;                 // tokens (or rows, with a position per head) of a block
+constexpr int kRows = 4;                       // rows per lane whose loads are all ahead of the arithmetic
+constexpr int kMaxTokens = 64;                 // tokens of a block
 
 struct RotaryArgs {
   const uint16_t* x;
@@ -27,20 +30,20 @@ struct RotaryArgs {
   int64_t p_sl, p_st, p_sh;
   const double* freq;
   uint32_t T, H, pairs;                        // pairs = rotary_dim / 2
-  uint32_t units, unit_heads, units_block;     // a unit: the heads that share a position (unit_heads = H, or 1); units per layer, per block
+  uint32_t tokens_block;                       // tokens of a block, heads sharing a position
   FastDiv div_h, div_pairs;
   float mscale, sign;
   bool copy;                                   // out is not x: channels behind rotary_dim are copied
 };
 
-// cosine and sine (times mscale, the sine with the direction's sign) of a position's pair
+constexpr double kTurn = 0.15915494309189535;   // 1 / (2 pi)
+
+// cosine and sine (times mscale, the sine with the direction's sign) of a position's pair; freq in turns
 __device__ __forceinline__ float2 turn_of(const RotaryArgs& a, int32_t pos, double freq) {
-  constexpr double kTurn = 0.15915494309189535;   // 1 / (2 pi)
-  double r = static_cast<double>(pos) * freq * kTurn;
+  double r = static_cast<double>(pos) * freq;
   r -= __builtin_rint(r);
-  float s, c;
-  sincospif(2.0f * static_cast<float>(r), &s, &c);
-  return make_float2(c * a.mscale, s * a.mscale * a.sign);
+  const float f = static_cast<float>(r);
+  return make_float2(__builtin_amdgcn_cosf(f) * a.mscale, __builtin_amdgcn_sinf(f) * (a.mscale * a.sign));
 }
 
 __device__ __forceinline__ void rotate(float& x, float& y, float2 cs) {
@@ -63,63 +66,122 @@ __device__ __forceinline__ uint4 rotate_pair8(uint4& lo, uint4 hi, const float2*
   return hi;
 }
 
-__device__ __forceinline__ uint4 rotate_piece(uint4 v, const float2* cs, uint32_t first, uint32_t pairs) {   // interleaved: 4 pairs of a piece
+__device__ __forceinline__ uint4 rotate_piece(uint4 v, const float2* cs, uint32_t first, uint32_t pairs) {   // interleaved: 4 pairs of a piece, the first of them `first`
   uint32_t* w = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i) {
     if (first + i < pairs) {
       float a = bf16lo(w[i]), b = bf16hi(w[i]);
-      rotate(a, b, cs[first + i]);
+      rotate(a, b, cs[i]);
       w[i] = pack_bf16x2(a, b);
     }
   }
   return v;
 }
 
-// LAYOUT half: rotary_dim is a multiple of 16
+// The pieces of lane j of a row: half layout (rotary_dim a multiple of 16) 8 j and 8 j + rotary_dim / 2 while there are pairs, then
+// two of the rest each.
+template <int LAYOUT>
+__device__ __forceinline__ bool pieces_of(const RotaryArgs& a, uint32_t j, uint32_t& c0, uint32_t& c1) {
+  if (LAYOUT == KVP_ROTARY_INTERLEAVED) {
+    c0 = 8 * j;
+    c1 = 64 + 8 * j;
+    return true;
+  }
+  const bool turns = 8 * j < a.pairs;
+  c0 = turns ? 8 * j : 2 * a.pairs + 16 * (j - a.pairs / 8);
+  c1 = turns ? c0 + a.pairs : c0 + 8;
+  return turns;
+}
+
+// One position for all heads of a token.
 template <int LAYOUT>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
   __shared__ float2 cs_s[kMaxTokens * 64];
-  const uint32_t l = blockIdx.y, unit0 = blockIdx.x * a.units_block, n_units = min(a.units_block, a.units - unit0);
-  const bool per_head = a.unit_heads == 1;     // a unit is a (token, head) row then
-  for (uint32_t i = threadIdx.x; i < n_units * a.pairs; i += kThreads) {
-    const uint32_t u = a.div_pairs.quot(i), p = i - u * a.pairs, unit = unit0 + u;
-    const uint32_t t = per_head ? a.div_h.quot(unit) : unit, h = per_head ? unit - t * a.H : 0;
-    const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
-    cs_s[u * 64 + p] = turn_of(a, pos, a.freq[p]);
+  const uint32_t l = blockIdx.y, token0 = blockIdx.x * a.tokens_block, tokens = min(a.tokens_block, a.T - token0);
+  for (uint32_t i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
+    const uint32_t u = a.div_pairs.quot(i), p = i - u * a.pairs;
+    const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(token0 + u) * a.p_st];
+    cs_s[u * 64 + p] = turn_of(a, pos, a.freq[p] * kTurn);
   }
   __syncthreads();
-  const uint32_t rows = n_units * a.unit_heads, row0 = unit0 * a.unit_heads;
+  const uint32_t rows = tokens * a.H;
   const uint16_t* x_l = a.x + static_cast<int64_t>(l) * a.x_sl;
   uint16_t* o_l = a.out + static_cast<int64_t>(l) * a.o_sl;
-  const uint32_t j = threadIdx.x & 7;
-  // pieces of this lane: half layout 8 j and 8 j + rotary_dim / 2 while j < rotary_dim / 16, then two of the rest
   uint32_t c0, c1;
-  bool turns;
-  if (LAYOUT == KVP_ROTARY_HALF) {
-    turns = 8 * j < a.pairs;
-    c0 = turns ? 8 * j : 2 * a.pairs + 16 * (j - a.pairs / 8);
-    c1 = turns ? c0 + a.pairs : c0 + 8;
-  } else {
-    turns = true;
-    c0 = 8 * j;
-    c1 = 64 + 8 * j;
-  }
+  const bool turns = pieces_of<LAYOUT>(a, threadIdx.x & 7, c0, c1);
   if (!turns && !a.copy) return;
-  for (uint32_t r = threadIdx.x >> 3; r < rows; r += kThreads / 8) {
-    const uint32_t row = row0 + r, t = a.div_h.quot(row), h = row - t * a.H;
-    const uint32_t u = per_head ? r : t - unit0;
-    const uint16_t* src = x_l + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
-    uint16_t* dst = o_l + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
-    uint4 v0 = *reinterpret_cast<const uint4*>(src + c0), v1 = *reinterpret_cast<const uint4*>(src + c1);
-    if (LAYOUT == KVP_ROTARY_HALF) {
-      if (turns) v1 = rotate_pair8(v0, v1, cs_s + u * 64 + c0);
-    } else {
-      v0 = rotate_piece(v0, cs_s + u * 64, c0 / 2, a.pairs);
-      v1 = rotate_piece(v1, cs_s + u * 64, c1 / 2, a.pairs);
+  for (uint32_t r0 = threadIdx.x >> 3; r0 < rows; r0 += kRows * kThreads / 8) {
+    uint4 v[kRows][2];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const uint32_t r = r0 + k * (kThreads / 8), u = a.div_h.quot(r), t = token0 + u, h = r - u * a.H;
+      if (r >= rows) continue;
+      const uint16_t* src = x_l + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
+      v[k][0] = load_stream16(src + c0);
+      v[k][1] = load_stream16(src + c1);
     }
-    *reinterpret_cast<uint4*>(dst + c0) = v0;
-    *reinterpret_cast<uint4*>(dst + c1) = v1;
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const uint32_t r = r0 + k * (kThreads / 8), u = a.div_h.quot(r), t = token0 + u, h = r - u * a.H;
+      if (r >= rows) continue;
+      if (LAYOUT == KVP_ROTARY_HALF) {
+        if (turns) v[k][1] = rotate_pair8(v[k][0], v[k][1], cs_s + u * 64 + c0);
+      } else {
+        v[k][0] = rotate_piece(v[k][0], cs_s + u * 64 + c0 / 2, c0 / 2, a.pairs);
+        v[k][1] = rotate_piece(v[k][1], cs_s + u * 64 + c1 / 2, c1 / 2, a.pairs);
+      }
+      uint16_t* dst = o_l + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
+      store_stream16(dst + c0, v[k][0]);
+      store_stream16(dst + c1, v[k][1]);
+    }
+  }
+}
+
+// A position for every row.
+
+template <int LAYOUT>
+__global__ __launch_bounds__(kThreads) void rotary_rows_kernel(const RotaryArgs a) {
+  const uint32_t l = blockIdx.y, j = threadIdx.x & 7, n_rows = a.T * a.H;
+  uint32_t c0, c1;
+  const bool turns = pieces_of<LAYOUT>(a, j, c0, c1);
+  if (!turns && !a.copy) return;
+  double f[8];   // of this lane's pairs, in turns
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t p = LAYOUT == KVP_ROTARY_HALF ? c0 + i : (i < 4 ? c0 / 2 + i : c1 / 2 + i - 4);
+    f[i] = turns && p < a.pairs ? a.freq[p] * kTurn : 0.0;
+  }
+  const uint32_t row0 = blockIdx.x * (kRows * kThreads / 8) + (threadIdx.x >> 3);
+  uint4 v[kRows][2];
+  int32_t pos[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const uint32_t row = row0 + k * (kThreads / 8), t = a.div_h.quot(row), h = row - t * a.H;
+    if (row >= n_rows) continue;
+    const uint16_t* src = a.x + static_cast<int64_t>(l) * a.x_sl + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
+    pos[k] = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
+    v[k][0] = load_stream16(src + c0);
+    v[k][1] = load_stream16(src + c1);
+  }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const uint32_t row = row0 + k * (kThreads / 8), t = a.div_h.quot(row), h = row - t * a.H;
+    if (row >= n_rows) continue;
+    if (turns) {
+      float2 cs[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) cs[i] = turn_of(a, pos[k], f[i]);
+      if (LAYOUT == KVP_ROTARY_HALF) {
+        v[k][1] = rotate_pair8(v[k][0], v[k][1], cs);
+      } else {
+        v[k][0] = rotate_piece(v[k][0], cs, c0 / 2, a.pairs);
+        v[k][1] = rotate_piece(v[k][1], cs + 4, c1 / 2, a.pairs);
+      }
+    }
+    uint16_t* dst = a.out + static_cast<int64_t>(l) * a.o_sl + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
+    store_stream16(dst + c0, v[k][0]);
+    store_stream16(dst + c1, v[k][1]);
   }
 }
 
@@ -134,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void rotary_any_kernel(const RotaryArgs a
   const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
   if (lane < a.pairs) {
     float p = __uint_as_float(static_cast<uint32_t>(src[lane]) << 16), q = __uint_as_float(static_cast<uint32_t>(src[lane + a.pairs]) << 16);
-    rotate(p, q, turn_of(a, pos, a.freq[lane]));
+    rotate(p, q, turn_of(a, pos, a.freq[lane] * kTurn));
     const uint32_t w = pack_bf16x2(p, q);
     dst[lane] = static_cast<uint16_t>(w);
     dst[lane + a.pairs] = static_cast<uint16_t>(w >> 16);
@@ -184,10 +246,16 @@ extern "C" int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int3
     rotary_any_kernel<<<dim3(static_cast<unsigned>(ceil_div(rows, kThreads / kWave)), layers), kThreads, 0, st>>>(a);
     return launch_status();
   }
-  a.unit_heads = pos_stride_h == 0 ? a.H : 1;
-  a.units = pos_stride_h == 0 ? a.T : a.T * a.H;
-  a.units_block = static_cast<uint32_t>(std::min<int64_t>(kMaxTokens, std::max<int64_t>(1, 128 / a.unit_heads)));
-  const dim3 grid(static_cast<unsigned>(ceil_div(a.units, a.units_block)), layers);
+  if (pos_stride_h != 0) {
+    const dim3 grid(static_cast<unsigned>(ceil_div(x->T * x->H, kRows * kThreads / 8)), layers);
+    if (layout == KVP_ROTARY_HALF)
+      rotary_rows_kernel<KVP_ROTARY_HALF><<<grid, kThreads, 0, st>>>(a);
+    else
+      rotary_rows_kernel<KVP_ROTARY_INTERLEAVED><<<grid, kThreads, 0, st>>>(a);
+    return launch_status();
+  }
+  a.tokens_block = static_cast<uint32_t>(std::min<int64_t>(kMaxTokens, std::max<int64_t>(1, 64 / x->H)));
+  const dim3 grid(static_cast<unsigned>(ceil_div(a.T, a.tokens_block)), layers);
   if (layout == KVP_ROTARY_HALF)
     rotary_kernel<KVP_ROTARY_HALF><<<grid, kThreads, 0, st>>>(a);
   else

@@ -45,15 +45,6 @@ __device__ __forceinline__ uint4 blend(uint4 m, uint4 a, uint4 b) {   // a where
   return make_uint4((a.x & m.x) | (b.x & ~m.x), (a.y & m.y) | (b.y & ~m.y), (a.z & m.z) | (b.z & ~m.z), (a.w & m.w) | (b.w & ~m.w));
 }
 
-template <int FMT>
-__device__ __forceinline__ uint32_t recode4(uint32_t w, float old, const PageQuantizer& q) {
-  float x[4];
-  decode4<FMT>(w, x);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] *= old;
-  return q.codes4<FMT>(x);
-}
-
 // What a page of a plane becomes: scale before and after, and whether its older codes are coded again.
 struct PageScale {
   float old, scale;

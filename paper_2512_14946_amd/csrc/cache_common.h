@@ -137,6 +137,16 @@ struct PageQuantizer {
   }
 };
 
+// four codes of an old scale on a new one
+template <int FMT>
+__device__ __forceinline__ uint32_t recode4(uint32_t w, float old, const PageQuantizer& q) {
+  float x[4];
+  decode4<FMT>(w, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] *= old;
+  return q.codes4<FMT>(x);
+}
+
 // largest value over the wave of a non-negative number per lane
 __device__ __forceinline__ float wave_max(float v) {
   uint32_t u = __float_as_uint(group_max(v, 16));

@@ -43,21 +43,44 @@ __global__ __launch_bounds__(kThreads) void evict_rank_kernel(const EvictArgs a,
   }
 }
 
+// What the slots of a destination page hold: pool cell, slot and scale of the token that moves there.
+struct Origins {
+  int64_t cell[128];
+  float scale[128];
+  int32_t slot[128];
+  int32_t start[129];     // first slot of every stretch of slots whose tokens lie in one page, and the number of live slots
+  int32_t count[2];       // stretches that begin in each wave's slots
+};
+
 template <int FMT>
+__device__ __forceinline__ float decode1(uint32_t code) {
+  if constexpr (FMT == KVP_CACHE_INT8)
+    return static_cast<float>(static_cast<int>(__builtin_amdgcn_sbfe(static_cast<int>(code), 0, 8)));
+  else
+    return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(code), 0);
+}
+
+template <int FMT, int ITEMS>
 __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (128 + 16)];   // values: [channel][slot], pitch bs + 16
-  __shared__ int64_t from_s[128];           // pool cell of a slot's old page
-  __shared__ int32_t slot_s[128];           // its old slot, -1: none
-  __shared__ float scale_s[128], max_s[4];
+  constexpr int bs = 16 * ITEMS, pitch = bs + 4;
+  __shared__ __attribute__((aligned(16))) uint8_t in_s[kHeadDim * pitch], out_s[kHeadDim * pitch];   // values: a page, and what moves: [channel][slot]
+  __shared__ Origins from;
+  __shared__ float max_s[4];
   const CacheArgs &s = a.src, &d = a.dst;
   const uint32_t rest = a.div_h.quot(blockIdx.x), h = blockIdx.x - rest * s.H;
   const uint32_t bp = a.div_pages.quot(rest), p = rest - bp * a.pages, b = bp >> 1, plane = bp & 1;
-  const uint32_t bs = 1u << s.bs_log2, n = evict_len(a, b), m = min(n, a.budget), bh = b * s.H + h, t0 = p << s.bs_log2;
-  if (threadIdx.x < bs) {
-    const uint32_t i = t0 + threadIdx.x;
-    int32_t t = -1;
+  const uint32_t n = evict_len(a, b), m = min(n, a.budget), bh = b * s.H + h, t0 = p * bs;
+  const int tid = static_cast<int>(threadIdx.x);
+  bool begins = false;
+  if (tid < bs) {
+    const uint32_t i = t0 + tid;
+    int32_t t = -1, before = -1;
     // entries below m are tokens of the sequence; clamped all the same
-    if (i < m) t = static_cast<int32_t>(min(static_cast<uint32_t>(a.kept[static_cast<int64_t>(bh) * a.k + i]), n - 1));
+    if (i < m) {
+      const int32_t* kept = a.kept + static_cast<int64_t>(bh) * a.k + i;
+      t = static_cast<int32_t>(min(static_cast<uint32_t>(kept[0]), n - 1));
+      if (tid > 0) before = static_cast<int32_t>(min(static_cast<uint32_t>(kept[-1]), n - 1));
+    }
     if (plane == 0 && i < a.budget) {
       if (a.keep_idx) a.keep_idx[static_cast<int64_t>(bh) * a.budget + i] = t;
       if (a.acc_out && t >= 0) a.acc_out[static_cast<int64_t>(bh) * a.acc_out_stride + i] = a.acc[static_cast<int64_t>(bh) * a.acc_stride + t];
@@ -65,83 +88,142 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
     if (i == 0 && h == 0 && plane == 0 && a.lens_out) a.lens_out[b] = static_cast<int32_t>(m);
     if (t >= 0) {
       const int64_t cell = static_cast<int64_t>(cache_page(s, b, static_cast<uint32_t>(t) >> s.bs_log2)) * s.H + h;
-      from_s[threadIdx.x] = cell;
-      scale_s[threadIdx.x] = (plane ? s.v_scales : s.k_scales)[cell];
-      t &= static_cast<int32_t>(bs - 1);
+      from.cell[tid] = cell;
+      from.scale[tid] = (plane ? s.v_scales : s.k_scales)[cell];
+      from.slot[tid] = t & (bs - 1);
+      begins = before < 0 || (before >> s.bs_log2) != (t >> s.bs_log2);
     }
-    slot_s[threadIdx.x] = t;
   }
   if (t0 >= m) return;
+  const int live = static_cast<int>(min(m - t0, static_cast<uint32_t>(bs)));
+  const uint64_t votes = __builtin_amdgcn_ballot_w64(begins);
+  if (tid < 128 && (tid & 63) == 0) from.count[tid >> 6] = __popcll(votes);
   __syncthreads();
-  const int live = static_cast<int>(min(m - t0, bs)), items = static_cast<int>(bs >> 4);
-  const uint8_t* codes = plane ? s.v_codes : s.k_codes;
-  uint2 raw[8];
-  float amax = 0.0f;
+  const int stretches = from.count[0] + (bs > 64 ? from.count[1] : 0);
+  if (begins) from.start[(tid >> 6 ? from.count[0] : 0) + __popcll(votes & ((1ull << (tid & 63)) - 1))] = tid;
+  if (tid == 0) from.start[stretches] = live;
+
+  const int64_t cell_out = static_cast<int64_t>(cache_page(d, b, p)) * d.H + h;
+  const int ch8 = (tid & 15) * 8;
+  if (plane == 0) {
+    uint2 raw[ITEMS];
+    float amax = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i >= items) break;
-    const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4), ch = static_cast<int>(threadIdx.x & 15) * 8;
-    raw[i] = make_uint2(0, 0);
-    if (slot < live) {
-      const uint8_t* at = codes + (from_s[slot] << (s.bs_log2 + 7));
-      const int old = slot_s[slot];
-      if (plane) {
-        uint32_t w[2];
+    for (int i = 0; i < ITEMS; ++i) {
+      const int slot = (tid >> 4) + 16 * i;
+      raw[i] = make_uint2(0, 0);
+      if (slot < live) raw[i] = load_stream8(s.k_codes + (from.cell[slot] << (s.bs_log2 + 7)) + from.slot[slot] * kHeadDim + ch8);
+    }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint8_t* c = at + ((ch + 4 * k) << s.bs_log2) + old;
-          w[k] = c[0] | (c[bs] << 8) | (c[2 * bs] << 16) | (static_cast<uint32_t>(c[3 * bs]) << 24);
-        }
-        raw[i] = make_uint2(w[0], w[1]);
-      } else {
-        raw[i] = *reinterpret_cast<const uint2*>(at + old * kHeadDim + ch);
-      }
+    for (int i = 0; i < ITEMS; ++i) {
+      const int slot = (tid >> 4) + 16 * i;
+      if (slot >= live) continue;
       float x[8];
       decode4<FMT>(raw[i].x, x);
       decode4<FMT>(raw[i].y, x + 4);
-      amax = fmaxf(amax, abs_max8(x) * scale_s[slot]);   // rounding is monotonic: the largest product is the product of the largest
+      amax = fmaxf(amax, abs_max8(x) * from.scale[slot]);   // rounding is monotonic: the largest product is the product of the largest
+    }
+    amax = block_max256(amax, max_s);
+    const float scale = amax / kCodeMax<FMT>;
+    const PageQuantizer q(scale);
+    if (tid == 0) d.k_scales[cell_out] = scale;
+    uint8_t* out = d.k_codes + (cell_out << (d.bs_log2 + 7)) + ch8;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int slot = (tid >> 4) + 16 * i;
+      if (slot < live)
+        *reinterpret_cast<uint2*>(out + slot * kHeadDim) = make_uint2(recode4<FMT>(raw[i].x, from.scale[slot], q), recode4<FMT>(raw[i].y, from.scale[slot], q));
+    }
+    return;
+  }
+
+  // Values lie channel by channel, so a token touches every 64 bytes of its page: pages are read whole, the next while this one's tokens
+  // are picked.  Few tokens per page (a quarter or less of what would fill it on the whole): byte by byte, all at once.
+  float amax = 0.0f;
+  __syncthreads();
+  if (stretches * 4 > live && stretches > 4) {
+    for (int i = tid; i < live * 16; i += kThreads) {
+      const int slot = i >> 4, ch = (i & 15) * 8;
+      const uint8_t* at = s.v_codes + (from.cell[slot] << (s.bs_log2 + 7)) + ch * bs + from.slot[slot];
+      uint32_t w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = at[k * bs];
+      float top = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        out_s[(ch + k) * pitch + slot] = static_cast<uint8_t>(w[k]);
+        top = fmaxf(top, fabsf(decode1<FMT>(w[k])));
+      }
+      amax = fmaxf(amax, top * from.scale[slot]);
+    }
+  } else {
+    uint4 page[(ITEMS + 1) / 2];
+    auto load = [&](int j) {
+      const uint8_t* at = s.v_codes + (from.cell[from.start[j]] << (s.bs_log2 + 7));
+#pragma unroll
+      for (int i = 0; i < (ITEMS + 1) / 2; ++i)
+        if (tid + i * kThreads < kHeadDim * ITEMS) page[i] = load_stream16(at + (tid + i * kThreads) * 16);
+    };
+    load(0);
+    const int c = tid & 127;
+    for (int j = 0; j < stretches; ++j) {
+#pragma unroll
+      for (int i = 0; i < (ITEMS + 1) / 2; ++i) {
+        const int k = tid + i * kThreads;
+        if (k >= kHeadDim * ITEMS) break;
+        uint32_t* to = reinterpret_cast<uint32_t*>(in_s + (k / ITEMS) * pitch + (k % ITEMS) * 16);
+        to[0] = page[i].x; to[1] = page[i].y; to[2] = page[i].z; to[3] = page[i].w;
+      }
+      __syncthreads();
+      if (j + 1 < stretches) load(j + 1);
+      const int first = from.start[j], last = from.start[j + 1];
+      float top = 0.0f;
+      for (int slot = first + (tid >> 7); slot < last; slot += 2) {
+        const uint32_t code = in_s[c * pitch + from.slot[slot]];
+        out_s[c * pitch + slot] = static_cast<uint8_t>(code);
+        top = fmaxf(top, fabsf(decode1<FMT>(code)));
+      }
+      amax = fmaxf(amax, top * from.scale[first]);   // one page, one scale
+      __syncthreads();
     }
   }
   amax = block_max256(amax, max_s);
   const float scale = amax / kCodeMax<FMT>;
   const PageQuantizer q(scale);
-  const int64_t cell = static_cast<int64_t>(cache_page(d, b, p)) * d.H + h;
-  if (threadIdx.x == 0) (plane ? d.v_scales : d.k_scales)[cell] = scale;
-  uint8_t* out = (plane ? d.v_codes : d.k_codes) + (cell << (d.bs_log2 + 7));
-  const int pitch = static_cast<int>(bs) + 16;
+  if (tid == 0) d.v_scales[cell_out] = scale;
+  uint8_t* out = d.v_codes + (cell_out << (d.bs_log2 + 7));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i >= items) break;
-    const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4), ch = static_cast<int>(threadIdx.x & 15) * 8;
-    if (slot >= live) continue;
-    float x[8];
-    decode4<FMT>(raw[i].x, x);
-    decode4<FMT>(raw[i].y, x + 4);
+  for (int i = 0; i < (ITEMS + 1) / 2; ++i) {
+    const int k = tid + i * kThreads, run = k % ITEMS, n_run = min(live - run * 16, 16);
+    if (k >= kHeadDim * ITEMS || n_run <= 0) continue;
+    const uint32_t* in = reinterpret_cast<const uint32_t*>(out_s + (k / ITEMS) * pitch + run * 16);
+    uint32_t w[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] *= scale_s[slot];
-    const uint2 w = make_uint2(q.codes4<FMT>(x), q.codes4<FMT>(x + 4));
-    if (plane == 0) {
-      *reinterpret_cast<uint2*>(out + slot * kHeadDim + ch) = w;
+    for (int j = 0; j < 4; ++j) {
+      float x[4];
+      decode4<FMT>(in[j], x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = 4 * j + e < n_run ? x[e] * from.scale[run * 16 + 4 * j + e] : 0.0f;
+      w[j] = q.codes4<FMT>(x);
+    }
+    uint8_t* at = out + (k / ITEMS) * bs + run * 16;
+    if (n_run == 16) {
+      *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        turn_s[(ch + k) * pitch + slot] = static_cast<uint8_t>(w.x >> (8 * k));
-        turn_s[(ch + 4 + k) * pitch + slot] = static_cast<uint8_t>(w.y >> (8 * k));
-      }
+      for (int e = 0; e < 16; ++e)
+        if (e < n_run) at[e] = static_cast<uint8_t>(w[e >> 2] >> (8 * (e & 3)));
     }
   }
-  if (plane == 0) return;
-  __syncthreads();
-  for (int i = static_cast<int>(threadIdx.x); i < kHeadDim * items; i += kThreads) {
-    const int ch = i >> (s.bs_log2 - 4), run = i & (items - 1), n_run = min(live - run * 16, 16);
-    if (n_run <= 0) continue;
-    uint8_t* at = out + (ch << s.bs_log2) + run * 16;
-    const uint8_t* from = turn_s + ch * pitch + run * 16;
-    if (n_run == 16) {
-      *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(from);
-    } else {
-      for (int k = 0; k < n_run; ++k) at[k] = from[k];
-    }
+}
+
+template <int FMT>
+void move_launch(const EvictArgs& a, dim3 grid, hipStream_t st) {
+  switch (a.src.bs_log2) {
+    case 4: evict_move_kernel<FMT, 1><<<grid, kThreads, 0, st>>>(a); break;
+    case 5: evict_move_kernel<FMT, 2><<<grid, kThreads, 0, st>>>(a); break;
+    case 6: evict_move_kernel<FMT, 4><<<grid, kThreads, 0, st>>>(a); break;
+    default: evict_move_kernel<FMT, 8><<<grid, kThreads, 0, st>>>(a); break;
   }
 }
 
@@ -217,8 +299,8 @@ extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64
   select_topk_launch(a.rank, rows, max_len, max_len, a.k, kept, base + w.rank + w.kept, st);
   const dim3 grid(static_cast<unsigned>(rows * 2 * pages));
   if (src->format == KVP_CACHE_INT8)
-    evict_move_kernel<KVP_CACHE_INT8><<<grid, kThreads, 0, st>>>(a);
+    move_launch<KVP_CACHE_INT8>(a, grid, st);
   else
-    evict_move_kernel<KVP_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
+    move_launch<KVP_CACHE_E4M3>(a, grid, st);
   return launch_status();
 }

@@ -307,16 +307,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
 }
 
 // What every token drew from all rows: drawn_t = sum over rows 2^(s_rt - bias_r).  A block owns 512 tokens of a (sequence, head), 64 per
-// wave, their keys as operands in registers; 32 query rows at a time are turned into operands in LDS once for all eight waves.
+// wave, their keys as operands in registers; 64 query rows at a time are turned into operands in LDS once for all eight waves
+// (32 at a time: too little work to cover what the rows' loads take).
 // S = Q K^T here: a lane has one token, sums over rows are its own, complete and formed in one order.
 constexpr int kSumWaves = 8;
 constexpr int kSumThreads = kSumWaves * kWave;
+constexpr int kSumRows = 64;
 
 template <int FMT>
 __global__ __launch_bounds__(kSumThreads, 2) void weights_rows_kernel(const AttendArgs a, uint32_t groups, FastDiv div_groups) {
-  __shared__ uint4 q_s[2][8 * 64];                                      // operands [channel step]
-  __shared__ __attribute__((aligned(16))) float qs_s[2][32], bias_s[2][32];
-  __shared__ __attribute__((aligned(16))) uint32_t limit_s[2][32];
+  __shared__ uint4 q_s[2][2][8 * 64];                                   // operands [row block][channel step]
+  __shared__ __attribute__((aligned(16))) float qs_s[2][kSumRows], bias_s[2][kSumRows];
+  __shared__ __attribute__((aligned(16))) uint32_t limit_s[2][kSumRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hb = lane >> 5, col = lane & 31;
   const uint32_t bh = div_groups.quot(blockIdx.x), t0 = (blockIdx.x - bh * groups) * (kSumWaves * kTileTokens), t = t0 + wave * kTileTokens;
   const uint32_t b = a.div_h.quot(bh), h = bh - b * a.c.H;
@@ -341,44 +343,50 @@ __global__ __launch_bounds__(kSumThreads, 2) void weights_rows_kernel(const Atte
       kf[tb][2 * j + 1] = decode8_half<FMT>(x.z, x.w);
     }
   }
-  // staging: 16 threads a row, eight channels each: channels 8 p ..+7 are step 2 (p / 4) + p mod 2 of lane half (p / 2) mod 2
-  const int srow = tid >> 4, p8 = tid & 15, step = 2 * (p8 >> 2) + (p8 & 1), half = (p8 >> 1) & 1;
-  const uint32_t tiles = (a.M + 31) / 32, tile_log2 = __builtin_ctz(a.tile_rows);
-  uint4 raw;
+  // staging: eight threads a row, sixteen channels each: 16 p ..+15 are steps 2 (p / 2) and the next of lane half p mod 2
+  const int srow = tid >> 3, p16 = tid & 7, step = 2 * (p16 >> 1), half = p16 & 1;
+  const uint32_t tiles = (a.M + kSumRows - 1) / kSumRows, tile_log2 = __builtin_ctz(a.tile_rows);
+  uint4 raw[2];
   float bias;
   auto load = [&](uint32_t i) {
-    const uint32_t row = i * 32 + srow, w = a.div_g.quot(row), head = h * a.G + (row - w * a.G);
-    raw = make_uint4(0, 0, 0, 0);
+    const uint32_t row = i * kSumRows + srow, w = a.div_g.quot(row), head = h * a.G + (row - w * a.G);
+    raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
     bias = INFINITY;
     if (row < a.M && static_cast<int32_t>(w) < m) {
-      raw = *reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh + p8 * 8);
+      const uint16_t* p = a.q + static_cast<int64_t>(b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh + p16 * 16;
+      raw[0] = *reinterpret_cast<const uint4*>(p);
+      raw[1] = *reinterpret_cast<const uint4*>(p + 8);
       // the tile that the attention launch put this row in, see rows_of
       const uint32_t tile = row >> tile_log2, cell = bh * a.row_tiles + (a.row_tiles - 1 - tile);
-      bias = a.row_bias[static_cast<int64_t>(cell) * a.tile_rows + (row - tile * a.tile_rows)];
+      bias = a.row_bias[static_cast<int64_t>(cell) * a.tile_rows + (row - (tile << tile_log2))];
     }
   };
   auto store = [&](int buf, uint32_t i) {
-    float x[8];
-    unpack_bf16x8(raw, x);
-    const float top = group_max(abs_max8(x), 16);
+    float x[16];
+    unpack_bf16x8(raw[0], x);
+    unpack_bf16x8(raw[1], x + 8);
+    const float top = group_max(fmaxf(abs_max8(x), abs_max8(x + 8)), 8);
     const int e = __builtin_amdgcn_frexp_expf(top);
     const float sign = a.scale2 < 0.0f ? -1.0f : 1.0f;
-    half8_t y;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = static_cast<_Float16>(ldexpf(x[k] * sign, -e));
-    q_s[buf][step * 64 + ((half * 32 + srow) ^ step)] = as_uint4(y);
-    if (p8 == 0) {
-      const uint32_t row = i * 32 + srow, w = a.div_g.quot(row);
+    for (int j = 0; j < 2; ++j) {
+      half8_t y;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = static_cast<_Float16>(ldexpf(x[8 * j + k] * sign, -e));
+      q_s[buf][srow >> 5][(step + j) * 64 + ((half * 32 + (srow & 31)) ^ (step + j))] = as_uint4(y);
+    }
+    if (p16 == 0) {
+      const uint32_t row = i * kSumRows + srow, w = a.div_g.quot(row);
       qs_s[buf][srow] = ldexpf(fabsf(a.scale2), e);
       bias_s[buf][srow] = bias;
       limit_s[buf][srow] = row < a.M && static_cast<int32_t>(w) < m ? seen_by(a, n, m, w) : 0u;
     }
   };
-  // the first 32 rows of which any sees a token of this block
+  // the first rows of which any sees a token of this block
   uint32_t first = 0;
   if (a.causal) {
     const int64_t w = static_cast<int64_t>(t0) + m - n;                // tokens of query w and later see token t0
-    if (w > 0) first = static_cast<uint32_t>(min(w * a.G, static_cast<int64_t>(a.M))) / 32;
+    if (w > 0) first = static_cast<uint32_t>(min(w * a.G, static_cast<int64_t>(a.M))) / kSumRows;
   }
   if (first < tiles) {
     load(first);
@@ -388,23 +396,24 @@ __global__ __launch_bounds__(kSumThreads, 2) void weights_rows_kernel(const Atte
   int buf = 0;
   for (uint32_t i = first; i < tiles; ++i, buf ^= 1) {
     if (i + 1 < tiles) load(i + 1);
-    const uint32_t w_first = a.div_g.quot(i * 32);
-    const uint32_t least = static_cast<int32_t>(a.div_g.quot(min(i * 32 + 31, a.M - 1))) < m && i * 32 + 31 < a.M ? seen_by(a, n, m, w_first) : 0u;
+    const uint32_t w_first = a.div_g.quot(i * kSumRows), last = i * kSumRows + kSumRows - 1;
+    const uint32_t least = last < a.M && static_cast<int32_t>(a.div_g.quot(last)) < m ? seen_by(a, n, m, w_first) : 0u;
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb) {
+    for (int rt = 0; rt < 4; ++rt) {
+      const int rb = rt >> 1, tb = rt & 1;   // row block, token block
       floatx16 s;
 #pragma unroll
       for (int k = 0; k < 16; ++k) s[k] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(q_s[buf][c * 64 + (lane ^ c)]), kf[tb][c], s, 0, 0, 0);
+      for (int c = 0; c < 8; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(q_s[buf][rb][c * 64 + (lane ^ c)]), kf[tb][c], s, 0, 0, 0);
       const uint32_t tok = t + 32 * tb + col;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 qs = *reinterpret_cast<const float4*>(&qs_s[buf][8 * g + 4 * hb]), bi = *reinterpret_cast<const float4*>(&bias_s[buf][8 * g + 4 * hb]);
+        const float4 qs = *reinterpret_cast<const float4*>(&qs_s[buf][32 * rb + 8 * g + 4 * hb]), bi = *reinterpret_cast<const float4*>(&bias_s[buf][32 * rb + 8 * g + 4 * hb]);
         float p[4] = {__builtin_amdgcn_exp2f(fmaf(s[4 * g], qs.x * ks[tb], -bi.x)), __builtin_amdgcn_exp2f(fmaf(s[4 * g + 1], qs.y * ks[tb], -bi.y)),
                       __builtin_amdgcn_exp2f(fmaf(s[4 * g + 2], qs.z * ks[tb], -bi.z)), __builtin_amdgcn_exp2f(fmaf(s[4 * g + 3], qs.w * ks[tb], -bi.w))};
         if (t + kTileTokens > least) {
-          const uint4 li = *reinterpret_cast<const uint4*>(&limit_s[buf][8 * g + 4 * hb]);
+          const uint4 li = *reinterpret_cast<const uint4*>(&limit_s[buf][32 * rb + 8 * g + 4 * hb]);
           p[0] = tok < li.x ? p[0] : 0.0f; p[1] = tok < li.y ? p[1] : 0.0f; p[2] = tok < li.z ? p[2] : 0.0f; p[3] = tok < li.w ? p[3] : 0.0f;
         }
         drawn[tb] += (p[0] + p[1]) + (p[2] + p[3]);

@@ -261,7 +261,8 @@ int32_t kvp_eval_configs_ex(const kvp_view* q_win, const kvp_view* k, const kvp_
  * may hold any bytes: no call reads a meaning into them.  Entries of lens are clamped into [0, max_blocks * bs] and
  * table entries into [0, num_blocks) when they are read, so no content of device memory can make a call fault.
  * Limits of every call that takes a cache: D = 128; bs 16, 32, 64 or 128; B * H, num_blocks * H and
- * max_blocks * bs below 2^31; B * H * max_blocks below 2^31; otherwise KVP_ERR_UNSUPPORTED / KVP_ERR_SHAPE. */
+ * max_blocks * bs below 2^31; B * H * max_blocks below 2^31; a launch takes fewer than 2^32 threads: B * H times the pages that
+ * one call may touch below 2^24 (append, read), 2^23 (evict); otherwise KVP_ERR_UNSUPPORTED / KVP_ERR_SHAPE. */
 enum { KVP_CACHE_INT8 = 0, KVP_CACHE_E4M3 = 1 };
 typedef struct {
   uint8_t* k_codes;           /* device [num_blocks][H][bs][D] */
@@ -297,23 +298,23 @@ int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, const kvp_v
  * m = q_lens[b], query token w < m of sequence b stands at position p = n - m + w and sees the tokens t < n, with
  * `causal` those of t <= p.  Query heads j*G .. j*G+G-1 (G = Hq / H) read head j:
  *     out[b][w][i] = sum over seen t of softmax_t(scale * q . k_t) v_t      (k_t, v_t: code * scale, not rounded)
- * A row that sees no token is zero.  Rows w >= m are not written.  q_lens: device int32 [B], entries clamped into
+ * A row that sees no token is zero.  Rows w >= m are neither read nor written; out must not overlap q.  q_lens: device int32 [B], entries clamped into
  * [0, W], or NULL: W.  W = 1 is a decode step.
  * With acc_out, the weight that every token drew, summed over the G heads and the query tokens, is added to a running sum:
  *     acc_out[b][j][t] = (acc_in ? acc_in[b][j][t] : 0) + sum over w, i of the probabilities,   t < n
- * (device fp32, rows acc_stride floats apart, sequence b and head j at row b * H + j; acc_in may be acc_out; entries
- * t >= n are left as they were; always the same bits for the same input).
+ * (device fp32, rows acc_stride floats apart, sequence b and head j at row b * H + j; acc_in may be acc_out,
+ * and must not overlap it otherwise; entries t >= n are left as they were; always the same bits for the same input).
  * max_len: an upper bound of lens that the host knows, 0 for max_blocks * bs; it fixes how the work is shared out and the
  * workspace, and a longer sequence is treated as if it had max_len tokens.  acc_stride >= max_len.
  * Arithmetic: queries are split exactly into a power of two per row and 16-bit values (what lies 2^-24 below the row's
  * largest element is rounded away), codes are exact in 16 bits, the products of both contractions run on the matrix cores
  * with fp32 accumulation, logits, statistics and sums are fp32, probabilities are rounded to fp16 for the product
  * with V (2^-11 relative, half of it below 2^-14 of the row's largest).  Finite q and cache contents, finite scale.
- * Limits: those of a cache; W * G below 2^24; grid and workspace sizes below 2^31 blocks. */
+ * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256) and B * H * max_len / 512 below 2^23. */
 int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,
                          const kvp_view* out, const float* acc_in, float* acc_out, int64_t acc_stride, int64_t max_len,
                          void* ws, size_t ws_bytes, void* stream);
-/* weights: whether acc_out is given; T: max_len */
+/* weights: whether acc_out is given; T: max_len.  A workspace for some T serves every smaller one. */
 size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t Hq, int64_t W, int64_t T, int32_t weights);
 
 /* Eviction by accumulated attention weight: of the n = min(lens[b], max_len) tokens of every (sequence, head), the
@@ -324,7 +325,7 @@ size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t Hq, int64_
  * indices, -1 behind m; acc_out (device fp32, rows acc_out_stride >= budget apart, may be NULL) the kept weights, entries
  * behind m are left as they were; lens_out (device int32 [B], may be NULL) m.  dst->lens is not read and may be lens_out; lens_out must not be
  * src->lens, acc_out must not overlap acc, and the pages that dst names must not be among those of src (both may lie in one pool).
- * acc: device fp32, rows acc_stride >= max_len apart; NaN is out of contract.  sink + recent <= budget (KVP_ERR_SHAPE);
+ * acc: device fp32, rows acc_stride >= max_len apart; NaN and infinity count as the largest finite number.  sink + recent <= budget (KVP_ERR_SHAPE);
  * dst->max_blocks * bs >= budget.  max_len as in kvp_cache_attend.  src and dst agree in B, H, bs and format. */
 int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64_t acc_stride, int64_t budget, int64_t sink, int64_t recent,
                         const kvp_cache* dst, int32_t* keep_idx, float* acc_out, int64_t acc_out_stride, int32_t* lens_out,
@@ -340,7 +341,8 @@ size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t T, int64_t 
  * h * pos_stride_h; a stride may be 0.  A keep list [L][H][k] (strides H*k, 1, k) gives every kept token of every
  * head its own; keys that were rotated at one position move to another by the difference.  The angle is formed and reduced in
  * double, sine and cosine and the rotation in fp32, the result rounded once to bf16.  out has the shape of x; it may be the same
- * view (in place), or must not overlap it.  rotary_dim even, 2 .. 128; L <= 65535, T and T * H below 2^31. */
+ * view (in place), or must not overlap it.  rotary_dim even, 2 .. 128; L <= 65535, T and T * H below 2^31 (KVP_ROTARY_HALF with rotary_dim no
+ * multiple of 16: 2^26). */
 enum { KVP_ROTARY_HALF = 0, KVP_ROTARY_INTERLEAVED = 1 };
 int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int32_t* positions, int64_t pos_stride_l,
                    int64_t pos_stride_t, int64_t pos_stride_h, const double* freq, int32_t rotary_dim, int32_t layout,

@@ -312,7 +312,7 @@ extern "C" int32_t kvp_cache_append(const kvp_cache* cache, const kvp_view* k, c
   // W rows behind any number of older ones touch at most this many pages; never more than there are
   const int64_t pages = std::min<int64_t>(cache->max_blocks, ceil_div(k->T + cache->bs - 1, cache->bs));
   const int64_t blocks = cache->B * cache->H * pages;
-  if (blocks >= (1ll << 31)) return KVP_ERR_SHAPE;
+  if (!fits_grid(blocks, kThreads)) return KVP_ERR_SHAPE;
   a.pages = static_cast<uint32_t>(pages);
   a.div_h = FastDiv(a.c.H);
   a.div_pages = FastDiv(a.pages);
@@ -347,7 +347,7 @@ extern "C" int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, 
   a.R = static_cast<uint32_t>(R);
   const int64_t pages = std::min<int64_t>(cache->max_blocks, ceil_div(R + cache->bs - 1, cache->bs));
   const int64_t blocks = cache->B * cache->H * pages;
-  if (blocks >= (1ll << 31)) return KVP_ERR_SHAPE;
+  if (!fits_grid(blocks, kThreads)) return KVP_ERR_SHAPE;
   a.pages = static_cast<uint32_t>(pages);
   a.div_h = FastDiv(a.c.H);
   a.div_pages = FastDiv(a.pages);

@@ -386,8 +386,12 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   if (acc_out && acc_stride < max_len) return KVP_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(q_lens) | reinterpret_cast<uintptr_t>(acc_in) | reinterpret_cast<uintptr_t>(acc_out)) & 3u) return KVP_ERR_ALIGN;
   const AttendPlan p = make_attend_plan(cache->B, cache->H, q->H, W, max_len, acc_out != nullptr);
-  if (p.cells * std::max(p.chunks, p.tile_rows) + p.cells * ceil_div(max_len, kSlice) >= (1ll << 31)) return KVP_ERR_SHAPE;
+  // blocks of both passes over the keys (512 threads at most), of the join and of the weights
+  if (!fits_grid(p.cells * p.chunks, 512) || !fits_grid(p.cells * (p.tile_rows + ceil_div(max_len, kSlice)), kThreads) ||
+      !fits_grid(cache->B * cache->H * ceil_div(max_len, 512), 512))
+    return KVP_ERR_SHAPE;
   if (p.bytes != 0 && (!ws || ws_bytes < p.bytes || !aligned16(ws))) return KVP_ERR_WORKSPACE;
+  if (out->ptr == q->ptr) return KVP_ERR_SHAPE;   // several blocks, and the weights' pass, read a query row
   AttendArgs a{};
   a.c = cache_args(cache);
   a.q = static_cast<const uint16_t*>(q->ptr);

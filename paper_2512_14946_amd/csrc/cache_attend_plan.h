@@ -36,12 +36,13 @@ inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, 
   p.row_tiles = ceil_div(M, p.tile_rows);
   p.cells = B * H * p.row_tiles;
   const int64_t step = kTileTokens * kAttendWaves;
-  int64_t n = std::min(std::max<int64_t>(1, 512 / p.cells), ceil_div(T, step));
+  const int64_t n = std::min(std::max<int64_t>(1, 512 / p.cells), ceil_div(T, step));
   p.chunk = ceil_div(ceil_div(T, n), step) * step;
   p.chunks = ceil_div(T, p.chunk);
-  const size_t stats = align256_bytes(static_cast<size_t>(p.cells) * p.chunks * p.tile_rows * 2 * sizeof(float));
+  // sized for n chunks, which grow with T where the rounded ones need not: scratch for a T serves every smaller one
+  const size_t stats = align256_bytes(static_cast<size_t>(p.cells) * n * p.tile_rows * 2 * sizeof(float));
   if (p.chunks > 1) {
-    p.out_bytes = align256_bytes(static_cast<size_t>(p.cells) * p.chunks * p.tile_rows * 128 * sizeof(float));
+    p.out_bytes = align256_bytes(static_cast<size_t>(p.cells) * n * p.tile_rows * 128 * sizeof(float));
     p.stat_bytes = stats;
   }
   // Weights need the final statistics of their rows, and then the logits once more.  Up to 16 rows they are kept (4 bytes a row and token,

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void evict_rank_kernel(const EvictArgs a,
     const uint32_t t = t0 + i * kThreads;
     if (t >= a.T) break;
     float x = -INFINITY;
-    if (t < n) x = t < a.sink || t + a.recent >= n ? INFINITY : acc[t];
+    if (t < n) x = t < a.sink || t + a.recent >= n ? INFINITY : fminf(acc[t], 3.402823466e38f);   // nothing above a protected token
     rank[t] = x;
   }
 }
@@ -267,9 +267,9 @@ extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64
   if ((reinterpret_cast<uintptr_t>(acc) | reinterpret_cast<uintptr_t>(keep_idx) | reinterpret_cast<uintptr_t>(acc_out) |
        reinterpret_cast<uintptr_t>(lens_out)) & 3u)
     return KVP_ERR_ALIGN;
-  if (lens_out == src->lens || dst->block_table == src->block_table) return KVP_ERR_SHAPE;
+  if (lens_out == src->lens || acc_out == acc || dst->block_table == src->block_table) return KVP_ERR_SHAPE;
   const int64_t rows = src->B * src->H, pages = ceil_div(budget, src->bs), groups = ceil_div(max_len, 1024);
-  if (rows * 2 * pages >= (1ll << 31) || rows * groups >= (1ll << 31)) return KVP_ERR_SHAPE;
+  if (!fits_grid(rows * 2 * pages, kThreads) || !fits_grid(rows * groups, kThreads)) return KVP_ERR_SHAPE;
   const EvictLayout w = evict_layout(src->B, src->H, max_len, budget);
   if (!ws || ws_bytes < w.total || !aligned16(ws)) return KVP_ERR_WORKSPACE;
   EvictArgs a{};

@@ -189,8 +189,8 @@ __global__ __launch_bounds__(kThreads) void rotary_rows_kernel(const RotaryArgs 
 // channels of a pair belong to one lane, so a row may be turned in place.
 __global__ __launch_bounds__(kThreads) void rotary_any_kernel(const RotaryArgs a) {
   const uint32_t l = blockIdx.y, row = blockIdx.x * (kThreads / kWave) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= a.T * a.H) return;
   const uint32_t t = a.div_h.quot(row), h = row - t * a.H;
-  if (t >= a.T) return;
   const uint16_t* src = a.x + static_cast<int64_t>(l) * a.x_sl + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
   uint16_t* dst = a.out + static_cast<int64_t>(l) * a.o_sl + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
   const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
@@ -243,6 +243,7 @@ extern "C" int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int3
   const unsigned layers = static_cast<unsigned>(x->L);
   if (layout == KVP_ROTARY_HALF && rotary_dim % 16) {
     const int64_t rows = x->T * x->H;
+    if (!fits_grid(ceil_div(rows, kThreads / kWave), kThreads)) return KVP_ERR_SHAPE;
     rotary_any_kernel<<<dim3(static_cast<unsigned>(ceil_div(rows, kThreads / kWave)), layers), kThreads, 0, st>>>(a);
     return launch_status();
   }

@@ -403,6 +403,12 @@ def _check(rc: int, what: str):
         raise KVPError(rc, what)
 
 
+def _torch_stream(stream, device):
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+
+
 def _workspace(ws, nbytes: int, device, stream=None):
     """(tensor kept alive by the caller, pointer, bytes).  A workspace allocated here is a temporary: when the
     call runs on a stream other than torch's current one, the allocator is told so that it does not hand the
@@ -412,7 +418,7 @@ def _workspace(ws, nbytes: int, device, stream=None):
             return None, None, 0
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         if stream is not None:
-            s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+            s = _torch_stream(stream, device)
             if s != torch.cuda.current_stream(device):
                 ws.record_stream(s)
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
@@ -701,7 +707,10 @@ def kvp_cache_attend(q: torch.Tensor, cache: KVCache, out: torch.Tensor | None =
     that every token drew.  max_len: an upper bound of lens, 0 for the capacity.  Rows behind q_lens[b] are not written."""
     cs = _cache(cache)
     if out is None:
-        out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if q_lens is not None:      # rows that no call writes, cleared on the stream that the call runs on
+            with torch.cuda.stream(_torch_stream(stream, q.device)):
+                out.zero_()
     _one_device(cache.k_codes, q, out, q_lens, acc_in, acc_out, ws)
     qv, ov = _view(q), _view(out)
     cap = cs.max_blocks * cs.bs

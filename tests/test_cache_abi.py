@@ -206,3 +206,32 @@ def test_rotary_frequencies_refuse():
                dict(rotary_dim=64, scaling="banded", factor=2.0, original=4096.0, low=4.0, high=4.0)):
         with pytest.raises(kvp.KVPError):
             kvp.kvp_rotary_frequencies(**kw)
+
+
+def test_results_that_would_overwrite_what_is_read_are_refused():
+    need = kvp.kvp_cache_attend_workspace_bytes(3, 2, 8, 4, 128, True)
+    assert attend(ws_bytes=need, acc_out=4096) == SHAPE                                # queries and results in one place
+    assert evict(acc_out=4096, out_stride=128) == SHAPE                                # weights in and out
+
+
+def test_launches_beyond_what_a_grid_takes_are_refused():
+    big = dict(num_blocks=1 << 20, max_blocks=1 << 20, table_stride=1 << 20, bs=16, B=16)
+    c = cache(**big)                                                                   # 2^25 pages of a head
+    k = view(L=16, T=1 << 24)
+    assert lib.kvp_cache_append(ref(c), ref(k), ref(k), None, None) == SHAPE
+    assert lib.kvp_cache_read(ref(c), None, ref(k), None, None) == SHAPE
+    assert evict(src=c, dst=cache(block_table=1 << 21, **big), budget=1 << 24, stride=1 << 24, ws_bytes=1 << 62) == SHAPE
+    wide = cache(B=1 << 22, num_blocks=1, max_blocks=1, table_stride=1)
+    assert attend(q=view(L=1 << 22, H=8), out=view(L=1 << 22, H=8, ptr=1 << 30), c=wide, ws_bytes=1 << 62) == SHAPE
+    assert rotary(x=view(T=1 << 24, H=8), rd=8) == SHAPE
+
+
+def test_a_workspace_serves_every_smaller_bound():
+    g = torch.Generator().manual_seed(1)
+    for B, H, G, W in [(1, 1, 1, 1), (1, 8, 4, 1), (3, 2, 7, 3), (2, 1, 1, 100), (1, 2, 4, 600), (64, 8, 8, 1)]:
+        for weights in (False, True):
+            before = 0
+            for T in sorted(torch.randint(1, 70000, (400,), generator=g).tolist() + [255, 256, 257, 512, 513, 768, 1024, 1025]):
+                need = kvp.kvp_cache_attend_workspace_bytes(B, H, H * G, W, T, weights)
+                assert need >= before, (B, H, G, W, T)
+                before = need

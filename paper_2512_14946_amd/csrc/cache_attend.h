@@ -19,7 +19,8 @@ struct AttendArgs {
   int64_t q_sb, q_sw, q_sh, o_sb, o_sw, o_sh;
   const int32_t* q_lens;
   uint32_t W, G, M, tile_rows, row_tiles, max_len, chunk, chunks;
-  FastDiv div_tiles, div_h, div_g, div_chunks;
+  uint32_t blocks, per_xcd;                 // blocks of the attention launch; of an XCD
+  FastDiv div_tiles, div_h, div_g, div_bh;  // div_bh: by the blocks of a (sequence, head)
   float scale2;                             // scale * log2(e)
   int32_t causal;
   float* part_out;                          // [cell][chunk][tile row][128] unnormalized, or null (one chunk)
@@ -38,6 +39,16 @@ struct Rows {
   int32_t m;                                // query tokens of the sequence
   uint32_t least, most;                     // tokens seen by the tile's first and last row (most: by any)
 };
+
+// Block of an attention launch -> its number in the order (sequence, head; chunk; row tile), its cell and its chunk.  Blocks reach the 8
+// XCDs in turn, so an XCD takes a run of them: the row tiles of a chunk share its keys and values in one L2.
+__device__ __forceinline__ bool block_of(const AttendArgs& a, uint32_t& cell, uint32_t& chunk) {
+  const uint32_t id = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+  const uint32_t bh = a.div_bh.quot(id), in_bh = id - bh * a.chunks * a.row_tiles;
+  chunk = a.div_tiles.quot(in_bh);
+  cell = bh * a.row_tiles + (in_bh - chunk * a.row_tiles);
+  return id < a.blocks;
+}
 
 __device__ __forceinline__ uint32_t seen_by(const AttendArgs& a, uint32_t n, int32_t m, uint32_t w) {
   if (!a.causal) return n;
@@ -80,7 +91,7 @@ __device__ __forceinline__ int64_t run_cell(const AttendArgs& a, uint32_t b, uin
 }
 
 // More than 16 query rows: attention of all chunks (to a.out, or partial results), and the weights of the tokens.
-void attend_rows_launch(const AttendArgs& a, int64_t blocks, int format, hipStream_t st);
+void attend_rows_launch(const AttendArgs& a, int format, hipStream_t st);
 void weights_rows_launch(const AttendArgs& a, int format, hipStream_t st);
 
 }  // namespace kvp

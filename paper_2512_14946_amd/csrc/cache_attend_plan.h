@@ -12,9 +12,10 @@ namespace kvp {
 
 constexpr int kTileTokens = 64;   // tokens a wave works on at a time
 constexpr int kTileRows = 16;     // query rows of a block that reads operands straight from memory
-constexpr int kFewRows = 32;      // rows up to which tiles of 16 are taken, see make_attend_plan
+constexpr int kFewRows = 96;      // rows up to which tiles of 16 are taken, see make_attend_plan
 constexpr int kManyRows = 256;    // ... of a block that shares its tiles by way of LDS
 constexpr int kAttendWaves = 4;
+constexpr int kUnits = 256;       // CUs
 
 struct AttendPlan {
   int64_t tile_rows, row_tiles;   // rows of a tile; tiles of the G * W rows of a (sequence, head)
@@ -29,14 +30,26 @@ inline size_t align256_bytes(size_t n) { return (n + 255) / 256 * 256; }
 inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, int64_t T, bool weights) {
   AttendPlan p{};
   const int64_t M = Hq / H * W, stride = ceil_div(T, kTileTokens) * kTileTokens;
-  // Tiles of 16 rows read every key and value once per tile, the wide ones once, but a wave has 32 rows and few rows leave most waves
-  // without.  Wide over 16-row time at 16 x 8 x 8192 keys: 1.42 (32 rows), 0.95 (40, 48), 0.83 (64), 0.63 (80), 0.46 (128); at 1 x 8 x 8192 1.35
-  // (32), 1.18 (40, 48), 1.16 (64), 0.87 (80): 33 to 64 rows are even on the whole, and few keys cost little either way.
+  // Tiles of 16 rows read and decode every code once per tile (by way of the L2 after the first), the wide ones once, but a wave has 32 rows and
+  // few rows leave most waves without.  16-row against wide tiles, us: 70, 132 (32 rows), 99, 139 (64), 137, 146 (96), 175, 154 (128) at
+  // 16 x 8 x 8192 keys; 40, 68, 55, 69, 76, 72, 90, 76 at 4 x 4 x 30000; 13, 20, 16, 21, 21, 23, 21, 25 at 1 x 8 x 8192.
   p.tile_rows = M <= kFewRows ? kTileRows : kManyRows;
   p.row_tiles = ceil_div(M, p.tile_rows);
   p.cells = B * H * p.row_tiles;
   const int64_t step = kTileTokens * kAttendWaves;
-  const int64_t n = std::min(std::max<int64_t>(1, 512 / p.cells), ceil_div(T, step));
+  // Chunks: the fewest of a cell that leave CUs idle for less than a fifth of the time, in rounds of a block per CU (a second block per CU adds
+  // partial results, and little that four loads in flight per lane do not do).  256 against 512 blocks, us: 61, 71 (16 x 8 x 8192 keys, 32 rows),
+  // 34, 40 (4 x 4 x 30000), 89, 90 (4 x 4 x 131072, 4 rows), 49, 62 (8 x 2048, 2048 rows); 480 against 192: 76, 87 (4 x 4 x 30000, 96 rows).
+  // More than a round only for chunks that outweigh their partial results: 1056 blocks in 5 rounds against 264 in 2: 146, 200 (33 x 8 x 12000, 4
+  // rows); but 45, 38 with chunks of 768 (130 x 2 x 2100), and 84, 78 with 2000 for 528 cells (33 x 8 x 4000, 28 rows).
+  const int64_t first = std::max<int64_t>(1, kUnits / p.cells);
+  const int64_t last = std::min(first + 8, std::max(first, T / (p.tile_rows != kTileRows ? 4096 : p.cells < kUnits ? 1024 : 2048)));
+  int64_t n = first;
+  for (int64_t i = first, best = 0; i <= last && best < 52; ++i) {
+    const int64_t full = i * p.cells * 64 / (ceil_div(i * p.cells, kUnits) * kUnits);   // how full the CUs are, of 64
+    if (full > best) best = full, n = i;
+  }
+  n = std::min(n, ceil_div(T, step));
   p.chunk = ceil_div(ceil_div(T, n), step) * step;
   p.chunks = ceil_div(T, p.chunk);
   // sized for n chunks, which grow with T where the rounded ones need not: scratch for a T serves every smaller one

@@ -63,11 +63,6 @@ __device__ __forceinline__ float load_query32(const uint16_t* row, int hb, bool 
   return ldexpf(fabsf(scale2), e);
 }
 
-struct RowsGrid {
-  uint32_t blocks, per_xcd;       // work items; per XCD (blocks reach the 8 XCDs in turn by their number)
-  FastDiv div_pair, div_tiles;    // by chunks * row tiles, by row tiles
-};
-
 // Barrier of the block that leaves loads from memory in flight.
 __device__ __forceinline__ void block_step() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -76,14 +71,11 @@ __device__ __forceinline__ void block_step() {
 }
 
 template <int FMT>
-__global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendArgs a, const RowsGrid grid) {
+__global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendArgs a) {
   __shared__ uint4 k_s[kBuffers][16 * kKeyPitch], v_s[kBuffers][16 * kValuePitch];   // operands: keys [token block][channel step], values [channel block][run]
   __shared__ __attribute__((aligned(16))) float ks_s[kBuffers][4], vs_s[kBuffers][4];   // scales of the runs, of the values their log2
-  // neighbouring work items share keys and values (the row tiles of a chunk): an XCD takes a run of them
-  const uint32_t id = (blockIdx.x & 7) * grid.per_xcd + (blockIdx.x >> 3);
-  if (id >= grid.blocks) return;
-  const uint32_t bh = grid.div_pair.quot(id), in_bh = id - bh * a.chunks * a.row_tiles, chunk = grid.div_tiles.quot(in_bh);
-  const uint32_t cell = bh * a.row_tiles + (in_bh - chunk * a.row_tiles);
+  uint32_t cell, chunk;
+  if (!block_of(a, cell, chunk)) return;
   const Rows r = rows_of(a, cell);
   const uint32_t t0 = chunk * a.chunk, t1 = min(r.most, t0 + a.chunk);
   if (a.chunks > 1 && t0 >= t1) return;
@@ -433,17 +425,12 @@ __global__ __launch_bounds__(kSumThreads, 2) void weights_rows_kernel(const Atte
 
 }  // namespace
 
-void attend_rows_launch(const AttendArgs& a, int64_t blocks, int format, hipStream_t st) {
-  RowsGrid g{};
-  g.blocks = static_cast<uint32_t>(blocks);
-  g.per_xcd = static_cast<uint32_t>(ceil_div(blocks, 8));
-  g.div_pair = FastDiv(a.chunks * a.row_tiles);
-  g.div_tiles = FastDiv(a.row_tiles);
-  const dim3 grid(g.per_xcd * 8);
+void attend_rows_launch(const AttendArgs& a, int format, hipStream_t st) {
+  const dim3 grid(a.per_xcd * 8);
   if (format == KVP_CACHE_INT8)
-    attend_rows_kernel<KVP_CACHE_INT8><<<grid, kThreads, 0, st>>>(a, g);
+    attend_rows_kernel<KVP_CACHE_INT8><<<grid, kThreads, 0, st>>>(a);
   else
-    attend_rows_kernel<KVP_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a, g);
+    attend_rows_kernel<KVP_CACHE_E4M3><<<grid, kThreads, 0, st>>>(a);
 }
 
 void weights_rows_launch(const AttendArgs& a, int format, hipStream_t st) {

@@ -27,14 +27,15 @@ def _plan(exe, B, H, G, W, T):
 
 
 def test_decode_steps_read_their_operands_straight_from_memory_and_prompts_share_them(plan):
-    for G, W in [(1, 1), (8, 1), (16, 1), (4, 8)]:
+    for G, W in [(1, 1), (8, 1), (16, 1), (4, 8), (8, 12)]:
         assert _plan(plan, 1, 8, G, W, 8192)[0] == 16
-    for G, W in [(1, 33), (4, 512), (7, 203)]:
+    for G, W in [(1, 97), (4, 512), (7, 203)]:
         assert _plan(plan, 1, 8, G, W, 8192)[0] == 256
 
 
 def test_few_cells_split_the_tokens(plan):
-    assert _plan(plan, 1, 1, 4, 1, 131072)[1] == 512          # 256 tokens a block at least
-    assert _plan(plan, 1, 8, 4, 1, 4096)[1] == 16
+    assert _plan(plan, 1, 1, 4, 1, 131072)[1] == 256          # a block per compute unit
+    assert _plan(plan, 1, 8, 4, 1, 4096)[1] == 16             # 256 tokens a block at least
     assert _plan(plan, 1, 8, 4, 1, 256)[1] == 1
-    assert _plan(plan, 64, 8, 8, 1, 12288)[1] == 1            # two blocks per compute unit without
+    assert _plan(plan, 4, 4, 4, 24, 30000)[1] == 5            # 192 blocks would leave a quarter of them idle
+    assert _plan(plan, 64, 8, 8, 1, 12288)[1] == 1

@@ -310,7 +310,7 @@ int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, const kvp_v
  * largest element is rounded away), codes are exact in 16 bits, the products of both contractions run on the matrix cores
  * with fp32 accumulation, logits, statistics and sums are fp32, probabilities are rounded to fp16 for the product
  * with V (2^-11 relative, half of it below 2^-14 of the row's largest).  Finite q and cache contents, finite scale.
- * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256) and B * H * max_len / 512 below 2^23. */
+ * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256) below 2^23, B * H * max_len / 128 below 2^24. */
 int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,
                          const kvp_view* out, const float* acc_in, float* acc_out, int64_t acc_stride, int64_t max_len,
                          void* ws, size_t ws_bytes, void* stream);

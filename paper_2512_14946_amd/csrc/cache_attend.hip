@@ -400,7 +400,7 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   const AttendPlan p = make_attend_plan(cache->B, cache->H, q->H, W, max_len, acc_out != nullptr);
   // blocks of both passes over the keys (512 threads at most), of the join and of the weights
   if (!fits_grid(p.cells * p.chunks, 512) || !fits_grid(p.cells * (p.tile_rows + ceil_div(max_len, kSlice)), kThreads) ||
-      !fits_grid(cache->B * cache->H * ceil_div(max_len, 512), 512))
+      !fits_grid(cache->B * cache->H * ceil_div(max_len, kSumTokens), kThreads))
     return KVP_ERR_SHAPE;
   if (p.bytes != 0 && (!ws || ws_bytes < p.bytes || !aligned16(ws))) return KVP_ERR_WORKSPACE;
   if (out->ptr == q->ptr) return KVP_ERR_SHAPE;   // several blocks, and the weights' pass, read a query row

@@ -15,6 +15,7 @@ constexpr int kTileRows = 16;     // query rows of a block that reads operands s
 constexpr int kFewRows = 96;      // rows up to which tiles of 16 are taken, see make_attend_plan
 constexpr int kManyRows = 256;    // ... of a block that shares its tiles by way of LDS
 constexpr int kAttendWaves = 4;
+constexpr int kSumTokens = 128;   // tokens of a block that sums the weights of many rows
 constexpr int kUnits = 256;       // CUs
 
 struct AttendPlan {

@@ -298,80 +298,98 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
           make_uint2(pack_bf16x2(o[c][4 * i] * inv, o[c][4 * i + 1] * inv), pack_bf16x2(o[c][4 * i + 2] * inv, o[c][4 * i + 3] * inv));
 }
 
-// What every token drew from all rows: drawn_t = sum over rows 2^(s_rt - bias_r).  A block owns 512 tokens of a (sequence, head), 64 per
-// wave, their keys as operands in registers; 64 query rows at a time are turned into operands in LDS once for all eight waves
-// (32 at a time: too little work to cover what the rows' loads take).
-// S = Q K^T here: a lane has one token, sums over rows are its own, complete and formed in one order.
-constexpr int kSumWaves = 8;
-constexpr int kSumThreads = kSumWaves * kWave;
+// What every token drew from all rows: drawn_t = sum over rows 2^(s_rt - bias_r).  A wave owns 32 tokens of a (sequence, head), their keys as
+// operands in registers; 64 query rows at a time are copied to LDS for the four waves of a block.  Codes of either format are exact in
+// bf16, so the rows need no conversion here.
+// S^T = K Q^T: a lane has one query row, whose bias it keeps, and 16 of the tokens; it sums every 32nd row of each, and the
+// lanes' sums are joined at the end, always in one order.
+// Bound by the latency of a stage (products, exponentials, barrier) and by how many blocks a CU holds.  Blocks of 128 tokens against 512 with 64 per
+// wave, whole call in us: 209, 350 (8 x 2048 keys, 8192 rows), 148, 178 (8 x 8192, 2048 rows), 180, 178 (4 x 30011, 1421), 920, 873 (8 x 32768, 4096).
+constexpr int kSumThreads = kSumTokens / 32 * kWave;
 constexpr int kSumRows = 64;
+constexpr int kSumPairs = kSumRows * 8 / kSumThreads;   // runs of 16 channels that a thread copies per stage
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+// eight codes -> bf16 (exact)
+template <int FMT>
+__device__ __forceinline__ bf16x8_t decode8_bf16(uint32_t w0, uint32_t w1) {
+  float x[8];
+  decode4<FMT>(w0, x);
+  decode4<FMT>(w1, x + 4);
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
+  return __builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3]));
+}
 
 template <int FMT>
 __global__ __launch_bounds__(kSumThreads, 2) void weights_rows_kernel(const AttendArgs a, uint32_t groups, FastDiv div_groups) {
   __shared__ uint4 q_s[2][2][8 * 64];                                   // operands [row block][channel step]
-  __shared__ __attribute__((aligned(16))) float qs_s[2][kSumRows], bias_s[2][kSumRows];
-  __shared__ __attribute__((aligned(16))) uint32_t limit_s[2][kSumRows];
+  __shared__ float bias_s[2][kSumRows];
+  __shared__ uint32_t limit_s[2][kSumRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hb = lane >> 5, col = lane & 31;
-  const uint32_t bh = div_groups.quot(blockIdx.x), t0 = (blockIdx.x - bh * groups) * (kSumWaves * kTileTokens), t = t0 + wave * kTileTokens;
+  const uint32_t bh = div_groups.quot(blockIdx.x), t0 = (blockIdx.x - bh * groups) * kSumTokens, t = t0 + wave * 32;
   const uint32_t b = a.div_h.quot(bh), h = bh - b * a.c.H;
   const uint32_t n = min(cache_len(a.c, b), a.max_len);
   if (t0 >= n) return;
   int32_t m = static_cast<int32_t>(a.W);
   if (a.q_lens) m = min(max(a.q_lens[b], 0), m);
 
-  // keys of this lane's two tokens: step 2 j + e takes channels 32 j + 16 hb + 8 e ..+7
-  half8_t kf[2][8];
-  float ks[2], drawn[2] = {0.0f, 0.0f};
+  // keys of two tokens: step 2 j + e takes channels 32 j + 16 hb + 8 e ..+7
+  bf16x8_t kf[8];
+  float f[2], drawn[16];   // factors of the runs of 16 tokens; sums: register v of token block tb at 16 tb + v
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb) {
-    const uint32_t tok = t + 32 * tb + col, run = tok & ~15u;
-    const int64_t cell = run_cell(a, b, h, run, n);
-    ks[tb] = a.c.k_scales[cell];
-    const uint8_t* p = a.c.k_codes + (cell << (a.c.bs_log2 + 7)) + (tok & ((1u << a.c.bs_log2) - 1)) * kHeadDim + hb * 16;
+  for (int i = 0; i < 16; ++i) drawn[i] = 0.0f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) f[u] = a.c.k_scales[run_cell(a, b, h, t + 16 * u, n)] * a.scale2;
+  {
+    const uint32_t tok = t + col, run = tok & ~15u;
+    const uint8_t* p = a.c.k_codes + (run_cell(a, b, h, run, n) << (a.c.bs_log2 + 7)) + (tok & ((1u << a.c.bs_log2) - 1)) * kHeadDim + hb * 16;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint4 x = *reinterpret_cast<const uint4*>(p + 32 * j);
-      kf[tb][2 * j] = decode8_half<FMT>(x.x, x.y);
-      kf[tb][2 * j + 1] = decode8_half<FMT>(x.z, x.w);
+      kf[2 * j] = decode8_bf16<FMT>(x.x, x.y);
+      kf[2 * j + 1] = decode8_bf16<FMT>(x.z, x.w);
     }
   }
-  // staging: eight threads a row, sixteen channels each: 16 p ..+15 are steps 2 (p / 2) and the next of lane half p mod 2
-  const int srow = tid >> 3, p16 = tid & 7, step = 2 * (p16 >> 1), half = p16 & 1;
   const uint32_t tiles = (a.M + kSumRows - 1) / kSumRows, tile_log2 = __builtin_ctz(a.tile_rows);
-  uint4 raw[2];
-  float bias;
+  uint4 raw[kSumPairs][2];
+  float bias = INFINITY;
+  uint32_t limit = 0;
   auto load = [&](uint32_t i) {
-    const uint32_t row = i * kSumRows + srow, w = a.div_g.quot(row), head = h * a.G + (row - w * a.G);
-    raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
-    bias = INFINITY;
-    if (row < a.M && static_cast<int32_t>(w) < m) {
-      const uint16_t* p = a.q + static_cast<int64_t>(b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh + p16 * 16;
-      raw[0] = *reinterpret_cast<const uint4*>(p);
-      raw[1] = *reinterpret_cast<const uint4*>(p + 8);
-      // the tile that the attention launch put this row in, see rows_of
-      const uint32_t tile = row >> tile_log2, cell = bh * a.row_tiles + (a.row_tiles - 1 - tile);
-      bias = a.row_bias[static_cast<int64_t>(cell) * a.tile_rows + (row - (tile << tile_log2))];
+#pragma unroll
+    for (int u = 0; u < kSumPairs; ++u) {      // eight threads a row, sixteen channels each
+      const int at = tid + u * kSumThreads;
+      const uint32_t row = i * kSumRows + (at >> 3), w = a.div_g.quot(row), head = h * a.G + (row - w * a.G);
+      raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+      if (row < a.M && static_cast<int32_t>(w) < m) {
+        const uint16_t* p = a.q + static_cast<int64_t>(b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh + (at & 7) * 16;
+        raw[u][0] = *reinterpret_cast<const uint4*>(p);
+        raw[u][1] = *reinterpret_cast<const uint4*>(p + 8);
+      }
+    }
+    if (wave == 0) {
+      const uint32_t row = i * kSumRows + lane, w = a.div_g.quot(row);
+      bias = INFINITY;
+      limit = 0;
+      if (row < a.M && static_cast<int32_t>(w) < m) {
+        // the tile that the attention launch put this row in, see rows_of
+        const uint32_t tile = row >> tile_log2, cell = bh * a.row_tiles + (a.row_tiles - 1 - tile);
+        bias = a.row_bias[static_cast<int64_t>(cell) * a.tile_rows + (row - (tile << tile_log2))];
+        limit = seen_by(a, n, m, w);
+      }
     }
   };
-  auto store = [&](int buf, uint32_t i) {
-    float x[16];
-    unpack_bf16x8(raw[0], x);
-    unpack_bf16x8(raw[1], x + 8);
-    const float top = group_max(fmaxf(abs_max8(x), abs_max8(x + 8)), 8);
-    const int e = __builtin_amdgcn_frexp_expf(top);
-    const float sign = a.scale2 < 0.0f ? -1.0f : 1.0f;
+  auto store = [&](int buf) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      half8_t y;
+    for (int u = 0; u < kSumPairs; ++u) {
+      const int at = tid + u * kSumThreads, row = at >> 3, step = 2 * ((at & 7) >> 1), half = at & 1;   // channels 16 p ..+15: steps 2 (p / 2) and the next, half p mod 2
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = static_cast<_Float16>(ldexpf(x[8 * j + k] * sign, -e));
-      q_s[buf][srow >> 5][(step + j) * 64 + ((half * 32 + (srow & 31)) ^ (step + j))] = as_uint4(y);
+      for (int j = 0; j < 2; ++j) q_s[buf][row >> 5][(step + j) * 64 + ((half * 32 + (row & 31)) ^ (step + j))] = raw[u][j];
     }
-    if (p16 == 0) {
-      const uint32_t row = i * kSumRows + srow, w = a.div_g.quot(row);
-      qs_s[buf][srow] = ldexpf(fabsf(a.scale2), e);
-      bias_s[buf][srow] = bias;
-      limit_s[buf][srow] = row < a.M && static_cast<int32_t>(w) < m ? seen_by(a, n, m, w) : 0u;
+    if (wave == 0) {
+      bias_s[buf][lane] = bias;
+      limit_s[buf][lane] = limit;
     }
   };
   // the first rows of which any sees a token of this block
@@ -382,44 +400,57 @@ __global__ __launch_bounds__(kSumThreads, 2) void weights_rows_kernel(const Atte
   }
   if (first < tiles) {
     load(first);
-    store(0, first);
+    store(0);
   }
   __syncthreads();
   int buf = 0;
+  auto sum = [&](auto mask_tag) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    floatx16 s[2];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) s[rb][k] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], __builtin_bit_cast(bf16x8_t, q_s[buf][rb][c * 64 + (lane ^ c)]), s[rb], 0, 0, 0);
+    }
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      const float row_bias = bias_s[buf][32 * rb + col];
+      const uint32_t row_limit = MASK ? limit_s[buf][32 * rb + col] : 0u;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[rb][k], f[k >> 3], -row_bias));
+        drawn[k] += !MASK || t + acc_row(hb, k) < row_limit ? p : 0.0f;
+      }
+    }
+  };
   for (uint32_t i = first; i < tiles; ++i, buf ^= 1) {
     if (i + 1 < tiles) load(i + 1);
     const uint32_t w_first = a.div_g.quot(i * kSumRows), last = i * kSumRows + kSumRows - 1;
     const uint32_t least = last < a.M && static_cast<int32_t>(a.div_g.quot(last)) < m ? seen_by(a, n, m, w_first) : 0u;
-#pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-      const int rb = rt >> 1, tb = rt & 1;   // row block, token block
-      floatx16 s;
-#pragma unroll
-      for (int k = 0; k < 16; ++k) s[k] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(q_s[buf][rb][c * 64 + (lane ^ c)]), kf[tb][c], s, 0, 0, 0);
-      const uint32_t tok = t + 32 * tb + col;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 qs = *reinterpret_cast<const float4*>(&qs_s[buf][32 * rb + 8 * g + 4 * hb]), bi = *reinterpret_cast<const float4*>(&bias_s[buf][32 * rb + 8 * g + 4 * hb]);
-        float p[4] = {__builtin_amdgcn_exp2f(fmaf(s[4 * g], qs.x * ks[tb], -bi.x)), __builtin_amdgcn_exp2f(fmaf(s[4 * g + 1], qs.y * ks[tb], -bi.y)),
-                      __builtin_amdgcn_exp2f(fmaf(s[4 * g + 2], qs.z * ks[tb], -bi.z)), __builtin_amdgcn_exp2f(fmaf(s[4 * g + 3], qs.w * ks[tb], -bi.w))};
-        if (t + kTileTokens > least) {
-          const uint4 li = *reinterpret_cast<const uint4*>(&limit_s[buf][32 * rb + 8 * g + 4 * hb]);
-          p[0] = tok < li.x ? p[0] : 0.0f; p[1] = tok < li.y ? p[1] : 0.0f; p[2] = tok < li.z ? p[2] : 0.0f; p[3] = tok < li.w ? p[3] : 0.0f;
-        }
-        drawn[tb] += (p[0] + p[1]) + (p[2] + p[3]);
-      }
-    }
-    if (i + 1 < tiles) store(buf ^ 1, i + 1);
+    if (t + 32 > least)
+      sum(std::true_type{});
+    else
+      sum(std::false_type{});
+    if (i + 1 < tiles) store(buf ^ 1);
     __syncthreads();
   }
+  // sums over the 32 lanes of a half: lane col ends up with drawn[col / 2]
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb) drawn[tb] += __shfl_xor(drawn[tb], 32);
-  const uint32_t tok = t + lane;            // lanes below 32 write the first 32 tokens, the others the rest
-  if (tok < n) {
+  for (int d = 16; d > 1; d /= 2)
+#pragma unroll
+    for (int i = 0; i < d / 2; ++i) {
+      const bool up = (lane & d) != 0;
+      const float mine = up ? drawn[i + d / 2] : drawn[i], other = up ? drawn[i] : drawn[i + d / 2];
+      drawn[i] = mine + __shfl_xor(other, d);
+    }
+  drawn[0] += __shfl_xor(drawn[0], 1);
+  const uint32_t tok = t + acc_row(hb, col >> 1);
+  if (tok < n && !(col & 1)) {
     const int64_t at = static_cast<int64_t>(bh) * a.acc_stride + tok;
-    a.acc_out[at] = (a.acc_in ? a.acc_in[at] : 0.0f) + (hb ? drawn[1] : drawn[0]);
+    a.acc_out[at] = (a.acc_in ? a.acc_in[at] : 0.0f) + drawn[0];
   }
 }
 
@@ -434,7 +465,7 @@ void attend_rows_launch(const AttendArgs& a, int format, hipStream_t st) {
 }
 
 void weights_rows_launch(const AttendArgs& a, int format, hipStream_t st) {
-  const int64_t groups = ceil_div(a.max_len, kSumWaves * kTileTokens), blocks = groups * a.c.B * a.c.H;
+  const int64_t groups = ceil_div(a.max_len, kSumTokens), blocks = groups * a.c.B * a.c.H;
   const FastDiv div(static_cast<uint32_t>(groups));
   const dim3 grid(static_cast<unsigned>(blocks));
   if (format == KVP_CACHE_INT8)

@@ -40,7 +40,7 @@ inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, 
   const int64_t step = kTileTokens * kAttendWaves;
   // Chunks: the fewest of a cell that leave CUs idle for less than a fifth of the time, in rounds of a block per CU (a second block per CU adds
   // partial results, and little that four loads in flight per lane do not do).  256 against 512 blocks, us: 61, 71 (16 x 8 x 8192 keys, 32 rows),
-  // 34, 40 (4 x 4 x 30000), 89, 90 (4 x 4 x 131072, 4 rows), 49, 62 (8 x 2048, 2048 rows); 480 against 192: 76, 87 (4 x 4 x 30000, 96 rows).
+  // 34, 40 (4 x 4 x 30000), 89, 90 (4 x 4 x 131072, 7 rows), 49, 62 (8 x 2048, 2048 rows); 480 against 192: 76, 87 (4 x 4 x 30000, 96 rows).
   // More than a round only for chunks that outweigh their partial results: 1056 blocks in 5 rounds against 264 in 2: 146, 200 (33 x 8 x 12000, 4
   // rows); but 45, 38 with chunks of 768 (130 x 2 x 2100), and 84, 78 with 2000 for 528 cells (33 x 8 x 4000, 28 rows).
   const int64_t first = std::max<int64_t>(1, kUnits / p.cells);

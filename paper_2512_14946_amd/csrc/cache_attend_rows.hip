@@ -1,11 +1,15 @@
-// kvp_cache_attend with more than 16 query rows per (sequence, head): prompts, chunks of prompts, several tokens at once.
+// kvp_cache_attend with many query rows per (sequence, head): prompts, chunks of prompts; and the weights of more than 16 rows.
 //
 // Bound by the matrix and vector pipes, no longer by the cache's bytes, so every code is turned into a half once per block: a block
-// of four waves owns 128 or 256 rows (32 or 64 per wave), stages 64 tokens at a time in LDS as operands of
-// v_mfma_f32_32x32x16_f16 (two buffers, one barrier per tile) and reads each operand for one or two products.
-// The arithmetic is that of cache_attend.hip: S^T = K Q^T leaves a lane with one query row and 32 of the 64 tokens, which are those that its
-// operand of O^T = V^T P^T takes if the values' tokens are dealt out in the same order, so probabilities stay in the lane.
-// A tile has four runs of 16 tokens; a run lies in one page, so scales are uniform over the wave.
+// of eight waves owns 256 rows, 32 per wave, and stages 64 tokens at a time in LDS as operands of v_mfma_f32_32x32x16_f16.
+// Four buffers, one barrier per tile.  The arithmetic is that of cache_attend.hip: S^T = K Q^T leaves a lane with one query row
+// and 32 of the 64 tokens, which are those that its operand of O^T = V^T P^T takes if the values' tokens are dealt out in the same order, so
+// probabilities stay in the lane.  A tile has four runs of 16 tokens; a run lies in one page, so scales are uniform over the wave.
+// A step multiplies the values of a tile and the keys of the next back to back (64 products), so that one wave's products run under
+// another's exponentials.  4 x 8 x 16384 keys, 4096 rows (causal): 1.03 ms, 1.04 PFLOP/s; a large library product of halves reaches 1.20
+// on this card.  A loop of bare products reaches about 2.0, so the rest is exponentials, the staging and the clock under that load.
+// Measured against it at the same sizes: 64 rows per wave, four waves 1.43 to 1.79 ms; two blocks of 128 rows per CU 1.21; halves of a
+// block in turn at products and exponentials, held apart by barriers, 1.10; products and exponentials interleaved by hand 1.09 to 1.15.
 //
 // LDS holds operands in the order of the lanes that read them (1 KB each, no conflicts), one or two slots further apart than that, so that
 // the writes, whose neighbouring lanes belong to different operands, spread over the banks too.
@@ -109,7 +113,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
   int32_t zero = 0;   // in a vector register, so that addresses built with it are vector addresses
   asm volatile("" : "+v"(zero));
   // Everything by way of vector loads, whose waits are counted: a scalar load is waited for at the next barrier, and a scale's
-  // cache line takes longer than a tile (1.10 -> 0.85 ms without staging at 4 x 8 x 16384 keys, 4096 rows).
+  // cache line takes longer than a tile.
   auto next_entry = [&](uint32_t t, int set) {
     entry[set] = a.c.table[static_cast<int64_t>(r.b) * a.c.table_stride + (min(t + 16 * run, r.n - 1) >> a.c.bs_log2) + zero];
   };
@@ -159,8 +163,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
   }
   floatx16 s[2];
   half8_t pf[4];
-  // The products of a step: values of a tile (PV), logits of the next (QK; behind the last tile, of whatever LDS holds: not used).  Operands come from LDS four at a time, two groups ahead of
-  // the four products that use them; consecutive products belong to different accumulators.
+  // The products of a step: values of a tile (PV), logits of the next (QK; behind the last tile, of whatever LDS holds: not used).
+  // Operands come from LDS four at a time, two groups ahead of the four products that use them; consecutive products belong to
+  // different accumulators.
   auto products = [&](auto pv_tag, int buf_v, int buf_k) {
     constexpr int kAhead = 3;
     constexpr int kPV = decltype(pv_tag)::value ? 4 : 0, kGroups = kPV + 4;
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
           s[j & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[g % kAhead][j], qf[2 * (g - kPV) + (j >> 1)], s[j & 1], 0, 0, 0);
       }
       if constexpr (g + kAhead - 1 < kGroups) __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);   // four reads of LDS,
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);                                  // then four products
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);                                           // then four products
     };
     fetch(std::integral_constant<int, 0>{});
     if constexpr (kAhead > 2) fetch(std::integral_constant<int, 1>{});

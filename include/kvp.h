@@ -284,7 +284,7 @@ typedef struct {
  *     scale = max(scale before, fl32(a / qmax))       otherwise;
  *     where that raised the scale, the codes before become rnd(fl32(fl32(code * scale before) / scale)),
  *     new codes are rnd(fl32(x / scale)), 0 when scale is 0 (IEEE binary32 quotients, rounded half to even to whole
- *     numbers or to e4m3; the sign of a zero code is not specified).
+ *     numbers or to e4m3; the sign of a zero code is not specified).  Finite k and v: one that is not spoils its page.
  * Slots behind the last token keep their bytes.  Pages that get tokens must belong to one sequence only (pages shared
  * between sequences may be full ones).  Graph capture: nothing but kernels is enqueued. */
 int32_t kvp_cache_append(const kvp_cache* cache, const kvp_view* k, const kvp_view* v, const int32_t* counts, void* stream);
@@ -308,8 +308,10 @@ int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, const kvp_v
  * workspace, and a longer sequence is treated as if it had max_len tokens.  acc_stride >= max_len.
  * Arithmetic: queries are split exactly into a power of two per row and 16-bit values (what lies 2^-24 below the row's
  * largest element is rounded away), codes are exact in 16 bits, the products of both contractions run on the matrix cores
- * with fp32 accumulation, logits, statistics and sums are fp32, probabilities are rounded to fp16 for the product
- * with V (2^-11 relative, half of it below 2^-14 of the row's largest).  Finite q and cache contents, finite scale.
+ * with fp32 accumulation, logits, statistics and sums are fp32; for the product with V a probability times its page's value
+ * scale is rounded to 11 bits (2^-11 relative) or to 2^-25 of the row's largest probability times the largest value scale,
+ * 2^-100 at least, whichever is coarser.  Finite q and cache contents, finite scale: a row that does not see a token is still
+ * spoiled by a value of it that is not finite.
  * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256) below 2^23, B * H * max_len / 128 below 2^24. */
 int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,
                          const kvp_view* out, const float* acc_in, float* acc_out, int64_t acc_stride, int64_t max_len,

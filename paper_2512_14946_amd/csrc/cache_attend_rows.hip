@@ -6,7 +6,7 @@
 // and 32 of the 64 tokens, which are those that its operand of O^T = V^T P^T takes if the values' tokens are dealt out in the same order, so
 // probabilities stay in the lane.  A tile has four runs of 16 tokens; a run lies in one page, so scales are uniform over the wave.
 // A step multiplies the values of a tile and the keys of the next back to back (64 products), so that one wave's products run under
-// another's exponentials.  4 x 8 x 16384 keys, 4096 rows (causal): 1.03 ms, 1.04 PFLOP/s; a large library product of halves reaches 1.20
+// another's exponentials.  4 x 8 x 16384 keys, 4096 rows (causal): 1.02 to 1.10 ms, 1.04 to 0.97 PFLOP/s; a large library product of halves reaches 1.20
 // on this card.  A loop of bare products reaches about 2.0, so the rest is exponentials, the staging and the clock under that load.
 // Measured against it at the same sizes: 64 rows per wave, four waves 1.43 to 1.79 ms; two blocks of 128 rows per CU 1.21; halves of a
 // block in turn at products and exponentials, held apart by barriers, 1.10; products and exponentials interleaved by hand 1.09 to 1.15.

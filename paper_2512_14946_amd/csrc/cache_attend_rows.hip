@@ -5,11 +5,12 @@
 // Four buffers, one barrier per tile.  The arithmetic is that of cache_attend.hip: S^T = K Q^T leaves a lane with one query row
 // and 32 of the 64 tokens, which are those that its operand of O^T = V^T P^T takes if the values' tokens are dealt out in the same order, so
 // probabilities stay in the lane.  A tile has four runs of 16 tokens; a run lies in one page, so scales are uniform over the wave.
-// A step multiplies the values of a tile and the keys of the next back to back (64 products), so that one wave's products run under
-// another's exponentials.  4 x 8 x 16384 keys, 4096 rows (causal): 1.02 to 1.10 ms, 1.04 to 0.97 PFLOP/s; a large library product of halves reaches 1.20
-// on this card.  A loop of bare products reaches about 2.0, so the rest is exponentials, the staging and the clock under that load.
-// Measured against it at the same sizes: 64 rows per wave, four waves 1.43 to 1.79 ms; two blocks of 128 rows per CU 1.21; halves of a
-// block in turn at products and exponentials, held apart by barriers, 1.10; products and exponentials interleaved by hand 1.09 to 1.15.
+// The halves of a block are half a tile apart, so that one's products run beside the other's exponentials.  4 x 8 x 16384 keys, 4096 rows
+// (causal): 1.00 to 1.08 ms on two cards, 1.06 to 0.99 PFLOP/s; a large library product of halves reaches 1.20.  Bound by power: 3500
+// cycles a tile where the products alone take 2048 and the exponentials and staging 2300, at 1.75 GHz of 2.4.
+// Measured against it at the same sizes, ms: both halves in step 1.03; 64 rows per wave, four waves 1.43 to 1.79; two blocks of 128 rows per CU
+// 1.21; halves held apart by two barriers a tile 1.09 to 1.13; products and exponentials interleaved by hand 1.09 to 1.15, products
+// and staging 1.07.
 //
 // LDS holds operands in the order of the lanes that read them (1 KB each, no conflicts), one or two slots further apart than that, so that
 // the writes, whose neighbouring lanes belong to different operands, spread over the banks too.
@@ -213,12 +214,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
   };
 
   block_step();
-  // One barrier per tile: four buffers keep a wave that is ahead from writing where one that is behind still reads.
-  if (tiles > 0) products(std::false_type{}, 0, 0);
-  auto step = [&](uint32_t i, int set) {
-    const uint32_t t = t0 + i * kTileTokens;
-    const int buf = i & (kBuffers - 1);
-    block_step();
+  auto softmax = [&](uint32_t t, int buf) {
     {
       const float4 k4 = *reinterpret_cast<const float4*>(ks_s[buf]), v4 = *reinterpret_cast<const float4*>(vs_s[buf]);
       const float v_u[4] = {v4.x, v4.y, v4.z, v4.w};
@@ -266,17 +262,40 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
       }
       sum += total;
     }
-    products(std::true_type{}, buf, (i + 1) & (kBuffers - 1));
+  };
+  auto stage = [&](uint32_t i, int set) {
+    const uint32_t t = t0 + i * kTileTokens;
     store_codes((i + 2) & (kBuffers - 1), t + 2 * kTileTokens, set);   // behind the last tile: into a buffer that is not read any more
     load_codes(t + 4 * kTileTokens, set);
     next_entry(t + 6 * kTileTokens, set);
   };
-  uint32_t i = 0;
-  for (; i + 1 < tiles; i += 2) {
-    step(i, 0);
-    step(i + 1, 1);
+  // A SIMD has a wave of either half of the block.  Between two barriers the early one works out the probabilities of tile i, then the products
+  // (values of i, keys of i + 1); the late one the products (values of i - 1, keys of i), then the probabilities: vector and matrix
+  // instructions of two waves run at the same time, and most of them do (3500 cycles a tile, 4170 with both in step; the clock
+  // falls under that load, and 1029 us become 1002).  Either half stages tile i + 2 behind what it does last, so four buffers are enough:
+  // i - 1, i, i + 1 are read while i + 2 is written.
+  const bool late = wave >= kWaves / 2;
+  if (tiles > 0) {
+    if (late) block_step();
+    products(std::false_type{}, 0, 0);
+    auto step = [&](uint32_t i, int set) {
+      if (!late) block_step();
+      softmax(t0 + i * kTileTokens, i & (kBuffers - 1));
+      if (late) {
+        stage(i, set);
+        block_step();
+      }
+      products(std::true_type{}, i & (kBuffers - 1), (i + 1) & (kBuffers - 1));
+      if (!late) stage(i, set);
+    };
+    uint32_t i = 0;
+    for (; i + 1 < tiles; i += 2) {
+      step(i, 0);
+      step(i + 1, 1);
+    }
+    if (i < tiles) step(i, 0);
+    if (!late) block_step();
   }
-  if (i < tiles) step(i, 0);
 
   const float z = sum + __shfl_xor(sum, 32), scale = __builtin_amdgcn_exp2f(vref);
   if (!valid) return;

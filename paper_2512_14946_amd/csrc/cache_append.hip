@@ -216,11 +216,11 @@ __device__ __forceinline__ uint4 restore8(uint32_t w0, uint32_t w1, float scale)
 
 template <int FMT, int ITEMS>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (16 * ITEMS + 16)];
+  __shared__ __attribute__((aligned(16))) uint8_t turn_s[kHeadDim * (16 * ITEMS + 4)];   // values: [channel][slot]
   const CacheArgs& c = a.c;
   const uint32_t bp = a.div_h.quot(blockIdx.x), h = blockIdx.x - bp * c.H, b = a.div_pages.quot(bp), p = bp - b * a.pages;
   constexpr uint32_t bs = 16 * ITEMS;
-  constexpr int pitch = 16 * ITEMS + 16;
+  constexpr int pitch = 16 * ITEMS + 4;
   const uint32_t first = a.first ? static_cast<uint32_t>(max(a.first[b], 0)) : 0u;
   const uint32_t end = min(cache_len(c, b), first + a.R), page = (first >> c.bs_log2) + p;
   if (page >= c.max_blocks) return;
@@ -247,27 +247,35 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(const ReadArgs a) 
 #pragma unroll
     for (int i = 0; i < (ITEMS + 1) / 2; ++i) {
       const int n = static_cast<int>(threadIdx.x + i * kThreads), ch = n / ITEMS, run = n % ITEMS;
-      if (n < kHeadDim * ITEMS) *reinterpret_cast<uint4*>(turn_s + ch * pitch + run * 16) = v[i];
+      uint32_t* to = reinterpret_cast<uint32_t*>(turn_s + ch * pitch + run * 16);
+      if (n < kHeadDim * ITEMS) to[0] = v[i].x, to[1] = v[i].y, to[2] = v[i].z, to[3] = v[i].w;
     }
-    __syncthreads();
   }
+  const int ch = static_cast<int>(threadIdx.x & 15) * 8;
+  if (a.dst[0]) {
+    uint16_t* dst = a.dst[0] + static_cast<int64_t>(b) * a.sb[0] + static_cast<int64_t>(h) * a.sh[0] + ch;
 #pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4), ch = static_cast<int>(threadIdx.x & 15) * 8;
-    if (slot < s0 || slot >= s1) continue;
-    if (a.dst[0])
-      store_stream16(a.dst[0] + static_cast<int64_t>(b) * a.sb[0] + static_cast<int64_t>(h) * a.sh[0] + (r0 + slot) * a.sr[0] + ch,
-                     restore8<FMT>(k[i].x, k[i].y, k_scale));
-    if (a.dst[1]) {
-      uint32_t w[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint8_t* at = turn_s + (ch + 4 * j) * pitch + slot;
-        w[j] = at[0] | (at[pitch] << 8) | (at[2 * pitch] << 16) | (static_cast<uint32_t>(at[3 * pitch]) << 24);
-      }
-      store_stream16(a.dst[1] + static_cast<int64_t>(b) * a.sb[1] + static_cast<int64_t>(h) * a.sh[1] + (r0 + slot) * a.sr[1] + ch,
-                     restore8<FMT>(w[0], w[1], v_scale));
+    for (int i = 0; i < ITEMS; ++i) {
+      const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4);
+      if (slot >= s0 && slot < s1) store_stream16(dst + (r0 + slot) * a.sr[0], restore8<FMT>(k[i].x, k[i].y, k_scale));
     }
+  }
+  if (!a.dst[1]) return;
+  __syncthreads();
+  // values: four slots of eight channels as words, turned in registers
+  uint16_t* dst = a.dst[1] + static_cast<int64_t>(b) * a.sb[1] + static_cast<int64_t>(h) * a.sh[1] + ch;
+#pragma unroll
+  for (int i = 0; i < (ITEMS + 3) / 4; ++i) {
+    const int slot = static_cast<int>((threadIdx.x + i * kThreads) >> 4) * 4;
+    if (slot >= s1 || slot + 4 <= s0) continue;   // s1: at most the page's slots
+    uint32_t w[8], lo[4], hi[4];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint32_t*>(turn_s + (ch + c) * pitch + slot);
+    turn4(w, lo);
+    turn4(w + 4, hi);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (slot + e >= s0 && slot + e < s1) store_stream16(dst + (r0 + slot + e) * a.sr[1], restore8<FMT>(lo[e], hi[e], v_scale));
   }
 }
 

@@ -5,8 +5,8 @@
 // Values are stored channel-major: a row's codes are turned in LDS, and whole runs of 16 slots of a channel go out as 16 bytes.
 // Read: the same blocks the other way.
 // Both move 2 + 1 bytes per element and are bound by HBM; a decode step (one row per sequence) is bound by latency.
-// 8 sequences x 8 heads, 4096 tokens at most, into 64-token pages and back: 59 us for both, 4.2 TB/s; 64 sequences x 8 heads, one token each: 5 us a call.
-// Both planes in a block: 59 us against 72 with a block per plane.
+// 8 sequences x 8 heads, 4096 tokens at most, into 64-token pages and back: 57 us for both, 4.4 TB/s; 64 sequences x 8 heads, one token each: 5 us a call.
+// Both planes in a block: 59 us against 72 with a block per plane; read by words of four slots: 57 (byte by byte LDS conflicts took half the read).
 
 #include "cache_common.h"
 

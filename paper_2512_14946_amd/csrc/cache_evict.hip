@@ -5,7 +5,7 @@
 // largest magnitude and codes them on the page's own scale.
 // Bound by the select for short contexts (8 heads x 4096 -> 2048 tokens: ranks 3 us, selection 6.5, move 7.5); for a batch by the values, of which
 // a token touches every 64 bytes of its page: 16 x 8 x 16384 (three quarters of that in the mean) -> 4916 tokens in 116 us, ranks and selection 18; the whole call and a read took
-// 305 us when values were gathered byte by byte, and take 200.
+// 305 us when values were gathered byte by byte, and take 198.
 // With ties toward the lowest index a sequence of n < budget tokens selects 0 .. budget - 1: its tokens, and then entries that the
 // last step knows to be none.
 

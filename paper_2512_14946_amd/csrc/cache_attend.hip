@@ -383,7 +383,9 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
 }  // namespace kvp
 
 extern "C" size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t Hq, int64_t W, int64_t T, int32_t weights) {
+  constexpr int64_t kMost = 1ll << 31, kRows = 1ll << 24;   // what a call accepts: nothing below overflows
   if (B <= 0 || H <= 0 || Hq <= 0 || Hq % H || W <= 0 || T <= 0) return 0;
+  if (B >= kMost || H >= kMost || B * H >= kMost || T >= kMost || W >= kRows || Hq / H >= kRows || Hq / H * W >= kRows) return 0;
   return kvp::make_attend_plan(B, H, Hq, W, T, weights != 0).bytes;
 }
 

@@ -249,7 +249,9 @@ EvictLayout evict_layout(int64_t B, int64_t H, int64_t T, int64_t budget) {
 }  // namespace kvp
 
 extern "C" size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t T, int64_t budget) {
+  constexpr int64_t kMost = 1ll << 31;   // what a call accepts: nothing below overflows
   if (B <= 0 || H <= 0 || T <= 0 || budget <= 0) return 0;
+  if (B >= kMost || H >= kMost || B * H >= kMost || T >= (1ll << 30) || budget >= kMost) return 0;
   return kvp::evict_layout(B, H, T, budget).total;
 }
 

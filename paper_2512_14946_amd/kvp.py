@@ -191,6 +191,9 @@ class KVCache:
     def nbytes(self) -> int:
         return 2 * self.k_codes.numel() + 8 * self.k_scales.numel()
 
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_c"}      # copies marshal their own tensors
+
 
 def alloc_cache(num_blocks: int, H: int, D: int, bs: int, block_table: torch.Tensor, lens: torch.Tensor, fmt: str = "int8") -> KVCache:
     """A cache of the sequences that block_table [B][max_blocks] and lens [B] describe, over a pool of its own."""

@@ -235,3 +235,25 @@ def test_a_workspace_serves_every_smaller_bound():
                 need = kvp.kvp_cache_attend_workspace_bytes(B, H, H * G, W, T, weights)
                 assert need >= before, (B, H, G, W, T)
                 before = need
+
+
+def test_sizes_that_no_call_accepts_are_none():
+    big = 1 << 32
+    assert kvp.kvp_cache_attend_workspace_bytes(big, big, big, 1, 4096, True) == 0     # a product that wraps to nothing
+    assert kvp.kvp_cache_attend_workspace_bytes(1, 1, 1, 1, 1 << 62, True) == 0
+    assert kvp.kvp_cache_attend_workspace_bytes(1, 1, 1 << 40, 1 << 40, 64, False) == 0
+    assert kvp.kvp_cache_evict_workspace_bytes(big, big, 64, 8) == 0 and kvp.kvp_cache_evict_workspace_bytes(1, 1, 1 << 62, 8) == 0
+    assert kvp.kvp_workspace_bytes(kvp.KVP_WS_CACHE_ATTEND, L=big, Hkv=big, Hq=big, W=1, T=64, method=0) == 0
+    assert kvp.kvp_workspace_bytes(kvp.KVP_WS_CACHE_EVICT, L=big, Hkv=big, T=64, k=8) == 0
+
+
+def test_copies_of_a_used_cache_refer_to_their_own_tensors(monkeypatch):
+    import copy
+    import pickle
+    monkeypatch.setattr(binding, "_one_device", lambda *ts: None)
+    c = kvp.alloc_cache(8, 2, 128, 16, torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    a = binding._cache(c)
+    for d in (copy.deepcopy(c), pickle.loads(pickle.dumps(c))):
+        b = binding._cache(d)
+        assert b.k_codes == d.k_codes.data_ptr() != a.k_codes and b.lens == d.lens.data_ptr() != a.lens
+    assert binding._cache(c) is a

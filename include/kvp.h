@@ -262,7 +262,7 @@ int32_t kvp_eval_configs_ex(const kvp_view* q_win, const kvp_view* k, const kvp_
  * table entries into [0, num_blocks) when they are read, so no content of device memory can make a call fault.
  * Limits of every call that takes a cache: D = 128; bs 16, 32, 64 or 128; B * H, num_blocks * H and
  * max_blocks * bs below 2^31; B * H * max_blocks below 2^31; a launch takes fewer than 2^32 threads: B * H times the pages that
- * one call may touch below 2^24 (append, read), 2^23 (evict); otherwise KVP_ERR_UNSUPPORTED / KVP_ERR_SHAPE. */
+ * one call may touch below 2^24; otherwise KVP_ERR_UNSUPPORTED / KVP_ERR_SHAPE. */
 enum { KVP_CACHE_INT8 = 0, KVP_CACHE_E4M3 = 1 };
 typedef struct {
   uint8_t* k_codes;           /* device [num_blocks][H][bs][D] */

@@ -1,11 +1,12 @@
 // kvp_cache_evict: of every (sequence, head) of an 8-bit paged cache the tokens that drew the most attention stay.
 //
 // Three steps: the weights become ranks (protected tokens +inf, what lies behind the last token -inf), kvp_select_topk's kernels take the
-// `budget` largest, ascending, and a block per (page of the destination, head, plane) gathers its tokens, reduces their
-// largest magnitude and codes them on the page's own scale.
-// Bound by the select for short contexts (8 heads x 4096 -> 2048 tokens: ranks 3 us, selection 6.5, move 7.5); for a batch by the values, of which
-// a token touches every 64 bytes of its page: 16 x 8 x 16384 (three quarters of that in the mean) -> 4916 tokens in 116 us, ranks and selection 18; the whole call and a read took
-// 305 us when values were gathered byte by byte, and take 198.
+// `budget` largest, ascending, and a block per (page of the destination, head) gathers its tokens, reduces their
+// largest magnitudes and codes them on the page's own scales.
+// Bound by the select for short contexts (8 heads x 4096 -> 2048 tokens: ranks 3 us, selection 6.5, move 7); for a batch by the values, of which
+// a token touches every 64 bytes of its page: 16 x 8 x 16384 (three quarters of that in the mean) -> 4916 tokens in 113 us, 4.6 TB/s of
+// whole pages, key rows and what is written; ranks and selection 18.  The whole call and a read took 305 us when values were gathered
+// byte by byte, and take 196.  A block per plane: 198, and 72 against 64 for 4 x 8 x 8192 -> 4096 tokens in 16-token pages.
 // With ties toward the lowest index a sequence of n < budget tokens selects 0 .. budget - 1: its tokens, and then entries that the
 // last step knows to be none.
 
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void evict_rank_kernel(const EvictArgs a,
 // What the slots of a destination page hold: pool cell, slot and scale of the token that moves there.
 struct Origins {
   int64_t cell[128];
-  float scale[128];
+  float k_scale[128], v_scale[128];
   int32_t slot[128];
   int32_t start[129];     // first slot of every stretch of slots whose tokens lie in one page, and the number of live slots
   int32_t count[2];       // stretches that begin in each wave's slots
@@ -68,10 +69,10 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
   constexpr int bs = 16 * ITEMS, pitch = bs + 4;
   __shared__ __attribute__((aligned(16))) uint8_t in_s[kHeadDim * pitch], out_s[kHeadDim * pitch];   // values: a page, and what moves: [channel][slot]
   __shared__ Origins from;
-  __shared__ float max_s[4];
+  __shared__ float max_s[2][4];
   const CacheArgs &s = a.src, &d = a.dst;
   const uint32_t rest = a.div_h.quot(blockIdx.x), h = blockIdx.x - rest * s.H;
-  const uint32_t bp = a.div_pages.quot(rest), p = rest - bp * a.pages, b = bp >> 1, plane = bp & 1;
+  const uint32_t b = a.div_pages.quot(rest), p = rest - b * a.pages;
   const uint32_t n = evict_len(a, b), m = min(n, a.budget), bh = b * s.H + h, t0 = p * bs;
   const int tid = static_cast<int>(threadIdx.x);
   bool begins = false;
@@ -84,15 +85,16 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
       t = static_cast<int32_t>(min(static_cast<uint32_t>(kept[0]), n - 1));
       if (tid > 0) before = static_cast<int32_t>(min(static_cast<uint32_t>(kept[-1]), n - 1));
     }
-    if (plane == 0 && i < a.budget) {
+    if (i < a.budget) {
       if (a.keep_idx) a.keep_idx[static_cast<int64_t>(bh) * a.budget + i] = t;
       if (a.acc_out && t >= 0) a.acc_out[static_cast<int64_t>(bh) * a.acc_out_stride + i] = a.acc[static_cast<int64_t>(bh) * a.acc_stride + t];
     }
-    if (i == 0 && h == 0 && plane == 0 && a.lens_out) a.lens_out[b] = static_cast<int32_t>(m);
+    if (i == 0 && h == 0 && a.lens_out) a.lens_out[b] = static_cast<int32_t>(m);
     if (t >= 0) {
       const int64_t cell = static_cast<int64_t>(cache_page(s, b, static_cast<uint32_t>(t) >> s.bs_log2)) * s.H + h;
       from.cell[tid] = cell;
-      from.scale[tid] = (plane ? s.v_scales : s.k_scales)[cell];
+      from.k_scale[tid] = s.k_scales[cell];
+      from.v_scale[tid] = s.v_scales[cell];
       from.slot[tid] = t & (bs - 1);
       begins = before < 0 || (before >> s.bs_log2) != (t >> s.bs_log2);
     }
@@ -108,15 +110,31 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
 
   const int64_t cell_out = static_cast<int64_t>(cache_page(d, b, p)) * d.H + h;
   const int ch8 = (tid & 15) * 8;
-  if (plane == 0) {
-    uint2 raw[ITEMS];
-    float amax = 0.0f;
+  uint2 raw[ITEMS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int slot = (tid >> 4) + 16 * i;
-      raw[i] = make_uint2(0, 0);
-      if (slot < live) raw[i] = load_stream8(s.k_codes + (from.cell[slot] << (s.bs_log2 + 7)) + from.slot[slot] * kHeadDim + ch8);
-    }
+  for (int i = 0; i < ITEMS; ++i) {
+    const int slot = (tid >> 4) + 16 * i;
+    raw[i] = make_uint2(0, 0);
+    if (slot < live) raw[i] = load_stream8(s.k_codes + (from.cell[slot] << (s.bs_log2 + 7)) + from.slot[slot] * kHeadDim + ch8);
+  }
+  __syncthreads();   // the stretches
+
+  // Values lie channel by channel, so a token touches every 64 bytes of its page: pages are read whole, the next while this one's tokens
+  // are picked.  Few tokens per page (a quarter or less of what would fill it on the whole): byte by byte, all at once.
+  float amax = 0.0f;
+  const bool bytes = stretches * 4 > live && stretches > 4;
+  uint4 page[(ITEMS + 1) / 2];
+  auto load = [&](int j) {
+    const uint8_t* at = s.v_codes + (from.cell[from.start[j]] << (s.bs_log2 + 7));
+#pragma unroll
+    for (int i = 0; i < (ITEMS + 1) / 2; ++i)
+      if (tid + i * kThreads < kHeadDim * ITEMS) page[i] = load_stream16(at + (tid + i * kThreads) * 16);
+  };
+  if (!bytes) load(0);
+
+  // keys, while the first page is on its way
+  {
+    float k_max = 0.0f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int slot = (tid >> 4) + 16 * i;
@@ -124,10 +142,10 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
       float x[8];
       decode4<FMT>(raw[i].x, x);
       decode4<FMT>(raw[i].y, x + 4);
-      amax = fmaxf(amax, abs_max8(x) * from.scale[slot]);   // rounding is monotonic: the largest product is the product of the largest
+      k_max = fmaxf(k_max, abs_max8(x) * from.k_scale[slot]);   // rounding is monotonic: the largest product is the product of the largest
     }
-    amax = block_max256(amax, max_s);
-    const float scale = amax / kCodeMax<FMT>;
+    k_max = block_max256(k_max, max_s[0]);
+    const float scale = k_max / kCodeMax<FMT>;
     const PageQuantizer q(scale);
     if (tid == 0) d.k_scales[cell_out] = scale;
     uint8_t* out = d.k_codes + (cell_out << (d.bs_log2 + 7)) + ch8;
@@ -135,16 +153,11 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
     for (int i = 0; i < ITEMS; ++i) {
       const int slot = (tid >> 4) + 16 * i;
       if (slot < live)
-        *reinterpret_cast<uint2*>(out + slot * kHeadDim) = make_uint2(recode4<FMT>(raw[i].x, from.scale[slot], q), recode4<FMT>(raw[i].y, from.scale[slot], q));
+        *reinterpret_cast<uint2*>(out + slot * kHeadDim) = make_uint2(recode4<FMT>(raw[i].x, from.k_scale[slot], q), recode4<FMT>(raw[i].y, from.k_scale[slot], q));
     }
-    return;
   }
 
-  // Values lie channel by channel, so a token touches every 64 bytes of its page: pages are read whole, the next while this one's tokens
-  // are picked.  Few tokens per page (a quarter or less of what would fill it on the whole): byte by byte, all at once.
-  float amax = 0.0f;
-  __syncthreads();
-  if (stretches * 4 > live && stretches > 4) {
+  if (bytes) {
     for (int i = tid; i < live * 16; i += kThreads) {
       const int slot = i >> 4, ch = (i & 15) * 8;
       const uint8_t* at = s.v_codes + (from.cell[slot] << (s.bs_log2 + 7)) + ch * bs + from.slot[slot];
@@ -157,17 +170,9 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
         out_s[(ch + k) * pitch + slot] = static_cast<uint8_t>(w[k]);
         top = fmaxf(top, fabsf(decode1<FMT>(w[k])));
       }
-      amax = fmaxf(amax, top * from.scale[slot]);
+      amax = fmaxf(amax, top * from.v_scale[slot]);
     }
   } else {
-    uint4 page[(ITEMS + 1) / 2];
-    auto load = [&](int j) {
-      const uint8_t* at = s.v_codes + (from.cell[from.start[j]] << (s.bs_log2 + 7));
-#pragma unroll
-      for (int i = 0; i < (ITEMS + 1) / 2; ++i)
-        if (tid + i * kThreads < kHeadDim * ITEMS) page[i] = load_stream16(at + (tid + i * kThreads) * 16);
-    };
-    load(0);
     const int c = tid & 127;
     for (int j = 0; j < stretches; ++j) {
 #pragma unroll
@@ -186,11 +191,11 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
         out_s[c * pitch + slot] = static_cast<uint8_t>(code);
         top = fmaxf(top, fabsf(decode1<FMT>(code)));
       }
-      amax = fmaxf(amax, top * from.scale[first]);   // one page, one scale
+      amax = fmaxf(amax, top * from.v_scale[first]);   // one page, one scale
       __syncthreads();
     }
   }
-  amax = block_max256(amax, max_s);
+  amax = block_max256(amax, max_s[1]);
   const float scale = amax / kCodeMax<FMT>;
   const PageQuantizer q(scale);
   if (tid == 0) d.v_scales[cell_out] = scale;
@@ -206,7 +211,7 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
       float x[4];
       decode4<FMT>(in[j], x);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = 4 * j + e < n_run ? x[e] * from.scale[run * 16 + 4 * j + e] : 0.0f;
+      for (int e = 0; e < 4; ++e) x[e] = 4 * j + e < n_run ? x[e] * from.v_scale[run * 16 + 4 * j + e] : 0.0f;
       w[j] = q.codes4<FMT>(x);
     }
     uint8_t* at = out + (k / ITEMS) * bs + run * 16;
@@ -274,7 +279,7 @@ extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64
     return KVP_ERR_ALIGN;
   if (lens_out == src->lens || acc_out == acc || dst->block_table == src->block_table) return KVP_ERR_SHAPE;
   const int64_t rows = src->B * src->H, pages = ceil_div(budget, src->bs), groups = ceil_div(max_len, 1024);
-  if (!fits_grid(rows * 2 * pages, kThreads) || !fits_grid(rows * groups, kThreads)) return KVP_ERR_SHAPE;
+  if (!fits_grid(rows * pages, kThreads) || !fits_grid(rows * groups, kThreads)) return KVP_ERR_SHAPE;
   const EvictLayout w = evict_layout(src->B, src->H, max_len, budget);
   if (!ws || ws_bytes < w.total || !aligned16(ws)) return KVP_ERR_WORKSPACE;
   EvictArgs a{};
@@ -302,7 +307,7 @@ extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64
   evict_rank_kernel<<<dim3(static_cast<unsigned>(rows * groups)), kThreads, 0, st>>>(a, static_cast<uint32_t>(groups),
                                                                                       FastDiv(static_cast<uint32_t>(groups)));
   select_topk_launch(a.rank, rows, max_len, max_len, a.k, kept, base + w.rank + w.kept, st);
-  const dim3 grid(static_cast<unsigned>(rows * 2 * pages));
+  const dim3 grid(static_cast<unsigned>(rows * pages));
   if (src->format == KVP_CACHE_INT8)
     move_launch<KVP_CACHE_INT8>(a, grid, st);
   else

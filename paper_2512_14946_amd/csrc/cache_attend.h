@@ -25,7 +25,7 @@ struct AttendArgs {
   int32_t causal;
   float* part_out;                          // [cell][chunk][tile row][128] unnormalized, or null (one chunk)
   float2* part_stat;                        // [cell][chunk][tile row] (reference, sum)
-  float* row_bias;                          // [cell][tile row] reference + log2(sum), +inf for an empty row: weights of more than 16 rows
+  float* row_bias;                          // [cell][tile row]: reference + log2(sum), +inf for an empty row: weights of more than 16 rows
   float* logits;                            // [cell][tile of 64 tokens][i][M][g][4], see the kernel: weights of a single row tile
   int64_t logit_stride;
   const float* acc_in;
@@ -90,7 +90,7 @@ __device__ __forceinline__ int64_t run_cell(const AttendArgs& a, uint32_t b, uin
   return entry_cell(a, h, run_entry(a, b, t, n));
 }
 
-// More than 16 query rows: attention of all chunks (to a.out, or partial results), and the weights of the tokens.
+// Tiles of kManyRows: attention of all chunks (to a.out, or partial results).  More than 16 query rows: the weights of the tokens.
 void attend_rows_launch(const AttendArgs& a, int format, hipStream_t st);
 void weights_rows_launch(const AttendArgs& a, int format, hipStream_t st);
 

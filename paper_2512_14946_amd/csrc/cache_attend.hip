@@ -11,14 +11,14 @@
 // halves hold them).  Logits are kept in base 2.  The reference that exponentials are taken against follows the maximum
 // lazily: it moves only when a logit exceeds it by 2^8, which P in halves and the sums in fp32 bear.
 //
-// This file: up to 96 query rows per (sequence, head) in tiles of 16, a decode step above all, bound by HBM.  A block's waves take a quarter of
-// its chunk each, with the loads of the next 64 tokens always in flight; partial results of chunks are joined by a second kernel.
+// This file: up to 128 query rows per (sequence, head) in tiles of 16 or 32, a decode step above all, bound by HBM.  A block's waves take a quarter
+// of its chunk each, with the loads of the next 64 tokens always in flight; partial results of chunks are joined by a second kernel.
 // The weights of the tokens need the final statistics of their rows: up to 16 rows the logits are kept and the second kernel sums them.
 // More rows, and the weights of more than 16: cache_attend_rows.hip.
 // 4 x 4 x 131072 tokens, 7 rows: 89 us, 6.06 TB/s (a copy reaches 6.5); 64 x 8 x 16384 (ragged, three quarters of that), 8 rows: 281 us, 5.7 TB/s,
-// and 435 with weights, of which storing the logits takes about 95 and reading them 58; 8 x 4096, 4 rows: 11 us, two launches and the latency of table, scale and code.
-// One product's worth of a tile of 16 rows feeds on 4 KB of codes, which are decoded once per tile: at 96 rows six times, so the
-// vector pipe, not HBM, holds 16 x 8 x 8192 tokens at 137 us.
+// and 435 with weights: the logits cost 12 us to keep, 78 to store beside the reads, and the joining kernel takes 54; 8 x 4096, 4 rows: 11 us,
+// two launches and the latency of length, table, scale and code.  Decoding holds several tiles: 16 x 8 x 8192 tokens take 54 us for 20 rows
+// and 118 for 96.
 
 #include <math.h>
 
@@ -92,25 +92,30 @@ __device__ __forceinline__ void load_values(const AttendArgs& a, int64_t cell, u
   for (int c = 0; c < 8; ++c) v[c] = load_codes16<SHARED>(p + (static_cast<uint32_t>(16 * c) << a.c.bs_log2));
 }
 
-template <int FMT>
-__device__ __forceinline__ void logits(const uint4 k[4][2], const half8_t qf[4], floatx4 s[4]) {
+template <int FMT, int R>
+__device__ __forceinline__ void logits(const uint4 k[4][2], const half8_t qf[R][4], floatx4 s[R][4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    s[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < R; ++u) s[u][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj) {
-      s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(decode8_half<FMT>(k[j][jj].x, k[j][jj].y), qf[2 * jj], s[j], 0, 0, 0);
-      s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(decode8_half<FMT>(k[j][jj].z, k[j][jj].w), qf[2 * jj + 1], s[j], 0, 0, 0);
+      const half8_t lo = decode8_half<FMT>(k[j][jj].x, k[j][jj].y), hi = decode8_half<FMT>(k[j][jj].z, k[j][jj].w);
+#pragma unroll
+      for (int u = 0; u < R; ++u) {
+        s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[u][2 * jj], s[u][j], 0, 0, 0);
+        s[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qf[u][2 * jj + 1], s[u][j], 0, 0, 0);
+      }
     }
   }
 }
 
-// LOGITS: they are kept for the weights (one row tile); SHARED: several row tiles
-template <int FMT, bool LOGITS, bool SHARED>
+// LOGITS: they are kept for the weights (one row tile); SHARED: several row tiles; R: groups of 16 rows, which share every code's decoding
+template <int FMT, bool LOGITS, bool SHARED, int R>
 __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs a) {
-  constexpr int kOutFloats = kTileRows * kOutPitch;
+  constexpr int kRows = 16 * R, kOutFloats = kRows * kOutPitch;
   __shared__ __attribute__((aligned(16))) float shared_s[kWaves * (LOGITS ? kKeptFloats : kOutFloats)];   // kept logits, then the waves' results
-  __shared__ float ref_s[kWaves][kTileRows], sum_s[kWaves][kTileRows], val_s[kWaves];
+  __shared__ float ref_s[kWaves][kRows], sum_s[kWaves][kRows], val_s[kWaves];
   uint32_t cell, chunk;
   if (!block_of(a, cell, chunk)) return;
   const Rows r = rows_of(a, cell);
@@ -118,13 +123,18 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
   const uint32_t t0 = chunk * a.chunk, t1 = min(r.most, t0 + a.chunk);
   if (a.chunks > 1 && t0 >= t1) return;      // the joining kernel knows which chunks there are
 
-  // this lane's query row
-  const uint32_t row = r.tile * kTileRows + col, w = a.div_g.quot(row), head = r.h * a.G + (row - w * a.G);
-  const bool valid = row < a.M && static_cast<int32_t>(w) < r.m;
-  half8_t qf[4];
-  const float qs = load_query(a.q + static_cast<int64_t>(r.b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh, g,
-                              valid, a.scale2, qf);
-  const uint32_t limit = valid ? seen_by(a, r.n, r.m, w) : 0u;
+  // this lane's query rows
+  half8_t qf[R][4];
+  float qs[R];
+  uint32_t limit[R];
+#pragma unroll
+  for (int u = 0; u < R; ++u) {
+    const uint32_t row = r.tile * kRows + 16 * u + col, w = a.div_g.quot(row), head = r.h * a.G + (row - w * a.G);
+    const bool valid = row < a.M && static_cast<int32_t>(w) < r.m;
+    qs[u] = load_query(a.q + static_cast<int64_t>(r.b) * a.q_sb + static_cast<int64_t>(w) * a.q_sw + static_cast<int64_t>(head) * a.q_sh, g, valid,
+                       a.scale2, qf[u]);
+    limit[u] = valid ? seen_by(a, r.n, r.m, w) : 0u;
+  }
 
   // Logits kept for the weights leave by way of LDS, some tiles at a time: loads that a wave requests after a store wait for that
   // store too, and a few stores in every tile cost 129 us of 409 at 64 x 8 x 12288 tokens and 8 rows.
@@ -132,10 +142,15 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
   const uint32_t keep = kKeptFloats / (a.M * kTileTokens);
   uint32_t n_kept = 0;
 
-  floatx4 o[8];
+  floatx4 o[R][8];
+  float ref[R], sum[R], vref = kLeastScale, inv_vref = 1.0f / kLeastScale;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) o[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  float ref = kLeast, sum = 0.0f, vref = kLeastScale, inv_vref = 1.0f / kLeastScale;
+  for (int u = 0; u < R; ++u) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[u][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    ref[u] = kLeast;
+    sum[u] = 0.0f;
+  }
 
   // The keys of the next tile are requested when this tile's are used up, its values likewise, with the scales and the table entries
   // of the tile after it in between: one set of registers, loads in flight all the time, and none waited for before its turn.
@@ -159,9 +174,12 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
   auto tile = [&](auto more_tag) {
     constexpr bool MORE = decltype(more_tag)::value;
     const uint32_t run = t + 16 * g;       // the 16 tokens of this lane
-    const float f = fmaxf(ks * qs, 0x1p-126f), vs_now = vs;   // never 0: what is masked stays -inf
-    floatx4 s[4];
-    logits<FMT>(k, qf, s);
+    const float vs_now = vs;
+    float f[R];
+#pragma unroll
+    for (int u = 0; u < R; ++u) f[u] = fmaxf(ks * qs[u], 0x1p-126f);   // never 0: what is masked stays -inf
+    floatx4 s[R][4];
+    logits<FMT, R>(k, qf, s);
     int64_t cell_v = 0;
     if constexpr (MORE) {
       cell_v = entry_cell(a, r.h, entry_v);
@@ -173,7 +191,9 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
     }
     if (t + kTileTokens > r.least) {         // some row does not see the whole tile
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i >> 2][i & 3] = run + i < limit ? s[i >> 2][i & 3] : -INFINITY;
+      for (int u = 0; u < R; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[u][i >> 2][i & 3] = run + i < limit[u] ? s[u][i >> 2][i & 3] : -INFINITY;
       if (t + kTileTokens > r.n) {           // bytes behind the last token may be anything: 0 * NaN is not 0
         const int live = static_cast<int>(min(max(static_cast<int64_t>(r.n) - run, int64_t(0)), int64_t(16)));
         uint32_t mask[4];
@@ -188,47 +208,62 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       if (col < static_cast<int>(a.M)) {
         float4* to = reinterpret_cast<float4*>(kept_s) + (n_kept * 4 * a.M + col) * 4 + g;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i * a.M * 4] = make_float4(s[i][0] * f, s[i][1] * f, s[i][2] * f, s[i][3] * f);
+        for (int i = 0; i < 4; ++i) to[i * a.M * 4] = make_float4(s[0][i][0] * f[0], s[0][i][1] * f[0], s[0][i][2] * f[0], s[0][i][3] * f[0]);
       }
       ++n_kept;
     }
-    float top = s[0][0];
+    float top[R];
+    bool moves = vs_now > kValueSlack * vref;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-    top *= f;                                // f > 0
-    if (__builtin_amdgcn_ballot_w64(top > ref + kSlack || vs_now > kValueSlack * vref)) {   // wave-uniform
-      float ref_new = fmaxf(ref, fmaxf(top, __shfl_xor(top, 16)));
-      ref_new = fmaxf(ref_new, __shfl_xor(ref_new, 32));
+    for (int u = 0; u < R; ++u) {
+      top[u] = s[u][0][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top[u] = fmaxf(top[u], s[u][i >> 2][i & 3]);
+      top[u] *= f[u];                        // f > 0
+      moves = moves || top[u] > ref[u] + kSlack;
+    }
+    if (__builtin_amdgcn_ballot_w64(moves)) {   // wave-uniform
       float v_new = fmaxf(vref, vs_now);
       v_new = fmaxf(v_new, __shfl_xor(v_new, 16));
       v_new = fmaxf(v_new, __shfl_xor(v_new, 32));
-      const float down = __builtin_amdgcn_exp2f(ref - ref_new), down_o = down * (vref / v_new);
-      sum *= down;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) o[c] *= down_o;
-      ref = ref_new;
+      for (int u = 0; u < R; ++u) {
+        float ref_new = fmaxf(ref[u], fmaxf(top[u], __shfl_xor(top[u], 16)));
+        ref_new = fmaxf(ref_new, __shfl_xor(ref_new, 32));
+        const float down = __builtin_amdgcn_exp2f(ref[u] - ref_new), down_o = down * (vref / v_new);
+        sum[u] *= down;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) o[u][c] *= down_o;
+        ref[u] = ref_new;
+      }
       vref = v_new;
       inv_vref = 1.0f / v_new;
     }
     // Probabilities times the page's share of the reference scale: the share goes into the exponent, and the sum of the tile is divided by it.
     // A share below 2^-60 leaves nothing of a half either way, and a page of zeros has none: both count as 2^-60.
-    const float log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f), off = log_share - ref;
-    float p[16], part = 0.0f;
+    const float log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f), per_share = __builtin_amdgcn_exp2f(-log_share);
+    half8_t pf[R][2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], f, off));
-      part += p[i];
+    for (int u = 0; u < R; ++u) {
+      const float off = log_share - ref[u];
+      float p[16], part = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[u][i >> 2][i & 3], f[u], off));
+        part += p[i];
+      }
+      sum[u] = fmaf(part, per_share, sum[u]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) pf[u][i >> 3][i & 7] = static_cast<_Float16>(p[i]);
     }
-    sum = fmaf(part, __builtin_amdgcn_exp2f(-log_share), sum);
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      half8_t pf;
+    for (int half = 0; half < 2; ++half)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pf[i] = static_cast<_Float16>(p[8 * half + i]);
+      for (int c = 0; c < 8; ++c) {
+        const half8_t x = half ? decode8_half<FMT>(v[c].z, v[c].w) : decode8_half<FMT>(v[c].x, v[c].y);
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(half ? decode8_half<FMT>(v[c].z, v[c].w) : decode8_half<FMT>(v[c].x, v[c].y), pf, o[c], 0, 0, 0);
-    }
+        for (int u = 0; u < R; ++u) o[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pf[u][half], o[u][c], 0, 0, 0);
+      }
     if constexpr (MORE) load_values<SHARED>(a, cell_v, run + kStep, lane, v);
     if constexpr (LOGITS) {
       if (!MORE || n_kept == keep) {
@@ -245,46 +280,52 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
   if (t < t_end) tile(std::false_type{});
   if constexpr (LOGITS) __syncthreads();   // the waves' results go where others may still keep logits
 
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
 #pragma unroll
-  for (int c = 0; c < 8; ++c) *reinterpret_cast<floatx4*>(&shared_s[wave * kOutFloats + col * kOutPitch + 16 * c + 4 * g]) = o[c];
-  if (g == 0) {
-    ref_s[wave][col] = ref;
-    sum_s[wave][col] = sum;
-    if (col == 0) val_s[wave] = vref;
+  for (int u = 0; u < R; ++u) {
+    sum[u] += __shfl_xor(sum[u], 16);
+    sum[u] += __shfl_xor(sum[u], 32);
+    const int in = 16 * u + col;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<floatx4*>(&shared_s[wave * kOutFloats + in * kOutPitch + 16 * c + 4 * g]) = o[u][c];
+    if (g == 0) {
+      ref_s[wave][in] = ref[u];
+      sum_s[wave][in] = sum[u];
+    }
   }
+  if (lane == 0) val_s[wave] = vref;
   __syncthreads();
   // the waves' results joined: thread -> (row, eight channels)
-  const int orow = threadIdx.x >> 4, ch = (threadIdx.x & 15) * 8;
-  float m = ref_s[0][orow];
 #pragma unroll
-  for (int i = 1; i < kWaves; ++i) m = fmaxf(m, ref_s[i][orow]);
-  float z = 0.0f, y[8] = {};
+  for (int u = 0; u < R; ++u) {
+    const int orow = 16 * u + (threadIdx.x >> 4), ch = (threadIdx.x & 15) * 8;
+    float m = ref_s[0][orow];
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    const float f = __builtin_amdgcn_exp2f(ref_s[i][orow] - m), fv = f * val_s[i];
-    z = fmaf(sum_s[i][orow], f, z);
+    for (int i = 1; i < kWaves; ++i) m = fmaxf(m, ref_s[i][orow]);
+    float z = 0.0f, y[8] = {};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = fmaf(shared_s[i * kOutFloats + orow * kOutPitch + ch + j], fv, y[j]);
+    for (int i = 0; i < kWaves; ++i) {
+      const float e = __builtin_amdgcn_exp2f(ref_s[i][orow] - m), ev = e * val_s[i];
+      z = fmaf(sum_s[i][orow], e, z);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = fmaf(shared_s[i * kOutFloats + orow * kOutPitch + ch + j], ev, y[j]);
+    }
+    const int64_t at = (static_cast<int64_t>(cell) * a.chunks + chunk) * kRows + orow;
+    const uint32_t row = r.tile * kRows + orow, w = a.div_g.quot(row);
+    if (a.part_stat && ch == 0) a.part_stat[at] = make_float2(m, z);
+    if (a.chunks > 1) {
+      if (row >= a.M) continue;
+      float4* dst = reinterpret_cast<float4*>(a.part_out + at * kHeadDim + ch);
+      dst[0] = make_float4(y[0], y[1], y[2], y[3]);
+      dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+      continue;
+    }
+    if (row >= a.M || static_cast<int32_t>(w) >= r.m) continue;
+    const float inv = z > 0.0f ? 1.0f / z : 0.0f;
+    if (a.row_bias && ch == 0) a.row_bias[static_cast<int64_t>(cell) * kRows + orow] = bias_of(m, z);
+    uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw + static_cast<int64_t>(r.h * a.G + (row - w * a.G)) * a.o_sh + ch;
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv),
+                                                pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
   }
-  const int64_t at = (static_cast<int64_t>(cell) * a.chunks + chunk) * kTileRows + orow;
-  if (a.part_stat && ch == 0) a.part_stat[at] = make_float2(m, z);
-  if (a.chunks > 1) {
-    if (r.tile * kTileRows + orow >= a.M) return;
-    float4* dst = reinterpret_cast<float4*>(a.part_out + at * kHeadDim + ch);
-    dst[0] = make_float4(y[0], y[1], y[2], y[3]);
-    dst[1] = make_float4(y[4], y[5], y[6], y[7]);
-    return;
-  }
-  const uint32_t r_out = r.tile * kTileRows + orow, w_out = a.div_g.quot(r_out);
-  if (r_out >= a.M || static_cast<int32_t>(w_out) >= r.m) return;
-  const float inv = z > 0.0f ? 1.0f / z : 0.0f;
-  if (a.row_bias && ch == 0) a.row_bias[static_cast<int64_t>(cell) * kTileRows + orow] = bias_of(m, z);
-  uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w_out) * a.o_sw +
-                  static_cast<int64_t>(r.h * a.G + (r_out - w_out * a.G)) * a.o_sh + ch;
-  *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv),
-                                              pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
 }
 
 // Row statistics over the chunks of a cell, by the 16 lanes that share `row`: (reference, sum); n chunks, `pitch` rows apart.
@@ -379,6 +420,16 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
     if (t + i < r.n) a.acc_out[at + i] = (a.acc_in ? a.acc_in[at + i] : 0.0f) + drawn[i];
 }
 
+template <int FMT>
+void few_rows_launch(const AttendArgs& a, dim3 grid, bool keep, int64_t tile_rows, hipStream_t st) {
+  if (tile_rows == kTileRows)
+    (keep              ? cache_attend_kernel<FMT, true, false, 1>
+     : a.row_tiles > 1 ? cache_attend_kernel<FMT, false, true, 1>
+                       : cache_attend_kernel<FMT, false, false, 1>)<<<grid, kThreads, 0, st>>>(a);
+  else
+    (a.row_tiles > 1 ? cache_attend_kernel<FMT, false, true, 2> : cache_attend_kernel<FMT, false, false, 2>)<<<grid, kThreads, 0, st>>>(a);
+}
+
 }  // namespace
 }  // namespace kvp
 
@@ -447,16 +498,12 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   const bool int8 = cache->format == KVP_CACHE_INT8;
   const dim3 grid(a.per_xcd * 8);
   const bool keep = p.logit_bytes != 0;
-  if (p.tile_rows > kTileRows)
+  if (p.tile_rows == kManyRows)
     attend_rows_launch(a, cache->format, st);
   else if (int8)
-    (keep              ? cache_attend_kernel<KVP_CACHE_INT8, true, false>
-     : p.row_tiles > 1 ? cache_attend_kernel<KVP_CACHE_INT8, false, true>
-                       : cache_attend_kernel<KVP_CACHE_INT8, false, false>)<<<grid, kThreads, 0, st>>>(a);
+    few_rows_launch<KVP_CACHE_INT8>(a, grid, keep, p.tile_rows, st);
   else
-    (keep              ? cache_attend_kernel<KVP_CACHE_E4M3, true, false>
-     : p.row_tiles > 1 ? cache_attend_kernel<KVP_CACHE_E4M3, false, true>
-                       : cache_attend_kernel<KVP_CACHE_E4M3, false, false>)<<<grid, kThreads, 0, st>>>(a);
+    few_rows_launch<KVP_CACHE_E4M3>(a, grid, keep, p.tile_rows, st);
   const uint32_t join_rows = std::min(a.M, a.tile_rows), slices = static_cast<uint32_t>(ceil_div(max_len, kSlice));
   const int64_t n_join = p.chunks > 1 ? p.cells * join_rows : 0, n_sum = p.logit_bytes ? p.cells * slices : 0;
   if (n_join + n_sum > 0)

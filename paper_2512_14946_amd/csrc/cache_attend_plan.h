@@ -11,8 +11,8 @@
 namespace kvp {
 
 constexpr int kTileTokens = 64;   // tokens a wave works on at a time
-constexpr int kTileRows = 16;     // query rows of a block that reads operands straight from memory
-constexpr int kFewRows = 96;      // rows up to which tiles of 16 are taken, see make_attend_plan
+constexpr int kTileRows = 16;     // query rows of a block that reads operands straight from memory, or twice that, see attend_tile_rows
+constexpr int kFewRows = 128;     // rows up to which those blocks are taken
 constexpr int kManyRows = 256;    // ... of a block that shares its tiles by way of LDS
 constexpr int kAttendWaves = 4;
 constexpr int kSumTokens = 128;   // tokens of a block that sums the weights of many rows
@@ -28,13 +28,27 @@ struct AttendPlan {
 
 inline size_t align256_bytes(size_t n) { return (n + 255) / 256 * 256; }
 
-inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, int64_t T, bool weights) {
+// Tokens from which M rows (17 .. 96) of n_bh (sequence, head)s take tiles of 32.
+inline int64_t wide_tiles_from(int64_t n_bh, int64_t M) { return std::max<int64_t>(1024, ceil_div(3 << 18, n_bh * ceil_div(M, kTileRows))); }
+
+// Rows of a tile.  Small tiles read and decode every code once per tile (by way of the L2 after the first), those of 256 once, but a wave
+// has 32 rows of them and few rows leave most waves without.  Tiles of 32 decode half as often as tiles of 16 and take longer to begin and end.  us,
+// tiles of 16 / 32 / 256:
+//   16 x 8 x 8192 keys   60 / 54 / 132 (20 rows), 99 / 71 / 139 (64), 138 / 118 / 146 (96), 175 / 126 / 154 (128), 171 (32) / 159 (160)
+//   4 x 4 x 30000        34 / 30 / 68,  52 / 40 / 69,  76 / 52 / 72,  90 / 63 / 75,  78 / 79
+//   1 x 8 x 32768        20 / 21 / -,   29 / 25 / -,   40 / 32 / - (88)
+//   1 x 8 x 8192         12 / 14 / 20,  14 / 15 / 21,  18 / 18 / 23,  21 / 18 / 25,  22 / 27
+//   64 x 8 x 512         19 / 22 / -,   35 / 40 / -,   50 / 59 / - (88)
+inline int64_t attend_tile_rows(int64_t n_bh, int64_t M, int64_t T) {
+  if (M <= kTileRows) return kTileRows;
+  if (M > kFewRows) return kManyRows;
+  return M > 96 || T >= wide_tiles_from(n_bh, M) ? 2 * kTileRows : kTileRows;
+}
+
+inline AttendPlan make_attend_plan_of(int64_t tile_rows, int64_t B, int64_t H, int64_t M, int64_t T, bool weights) {
   AttendPlan p{};
-  const int64_t M = Hq / H * W, stride = ceil_div(T, kTileTokens) * kTileTokens;
-  // Tiles of 16 rows read and decode every code once per tile (by way of the L2 after the first), the wide ones once, but a wave has 32 rows and
-  // few rows leave most waves without.  16-row against wide tiles, us: 70, 132 (32 rows), 99, 139 (64), 137, 146 (96), 175, 154 (128) at
-  // 16 x 8 x 8192 keys; 40, 68, 55, 69, 76, 72, 90, 76 at 4 x 4 x 30000; 13, 20, 16, 21, 21, 23, 21, 25 at 1 x 8 x 8192.
-  p.tile_rows = M <= kFewRows ? kTileRows : kManyRows;
+  const int64_t stride = ceil_div(T, kTileTokens) * kTileTokens;
+  p.tile_rows = tile_rows;
   p.row_tiles = ceil_div(M, p.tile_rows);
   p.cells = B * H * p.row_tiles;
   const int64_t step = kTileTokens * kAttendWaves;
@@ -43,8 +57,9 @@ inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, 
   // 34, 40 (4 x 4 x 30000), 89, 90 (4 x 4 x 131072, 7 rows), 49, 62 (8 x 2048, 2048 rows); 480 against 192: 76, 87 (4 x 4 x 30000, 96 rows).
   // More than a round only for chunks that outweigh their partial results: 1056 blocks in 5 rounds against 264 in 2: 146, 200 (33 x 8 x 12000, 4
   // rows); but 45, 38 with chunks of 768 (130 x 2 x 2100), and 84, 78 with 2000 for 528 cells (33 x 8 x 4000, 28 rows).
+  // (Times of tiles of 16 and 256.)
   const int64_t first = std::max<int64_t>(1, kUnits / p.cells);
-  const int64_t last = std::min(first + 8, std::max(first, T / (p.tile_rows != kTileRows ? 4096 : p.cells < kUnits ? 1024 : 2048)));
+  const int64_t last = std::min(first + 8, std::max(first, T / (p.tile_rows == kManyRows ? 4096 : p.cells < kUnits ? 1024 : 2048)));
   int64_t n = first;
   for (int64_t i = first, best = 0; i <= last && best < 52; ++i) {
     const int64_t full = i * p.cells * 64 / (ceil_div(i * p.cells, kUnits) * kUnits);   // how full the CUs are, of 64
@@ -69,6 +84,15 @@ inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, 
     p.row_bytes = align256_bytes(static_cast<size_t>(p.cells) * p.tile_rows * sizeof(float));
   }
   p.bytes = p.out_bytes + p.stat_bytes + p.row_bytes + p.logit_bytes;
+  return p;
+}
+
+inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, int64_t T, bool weights) {
+  const int64_t M = Hq / H * W, rows = attend_tile_rows(B * H, M, T);
+  AttendPlan p = make_attend_plan_of(rows, B, H, M, T, weights);
+  // scratch that serves every smaller T: the smaller tiles of fewer tokens too
+  if (rows == 2 * kTileRows && M <= 96)
+    p.bytes = std::max(p.bytes, make_attend_plan_of(kTileRows, B, H, M, wide_tiles_from(B * H, M) - 1, weights).bytes);
   return p;
 }
 

@@ -228,7 +228,8 @@ def test_launches_beyond_what_a_grid_takes_are_refused():
 
 def test_a_workspace_serves_every_smaller_bound():
     g = torch.Generator().manual_seed(1)
-    for B, H, G, W in [(1, 1, 1, 1), (1, 8, 4, 1), (3, 2, 7, 3), (2, 1, 1, 100), (1, 2, 4, 600), (64, 8, 8, 1), (33, 8, 4, 1), (5, 8, 8, 5), (2, 8, 4, 1100)]:
+    for B, H, G, W in [(1, 1, 1, 1), (1, 8, 4, 1), (3, 2, 7, 3), (2, 1, 1, 100), (1, 2, 4, 600), (64, 8, 8, 1), (33, 8, 4, 1), (5, 8, 8, 5), (2, 8, 4, 1100), (43, 1, 3, 15), (1, 8, 20, 1),
+                       (7, 8, 12, 8), (2, 8, 16, 7)]:
         for weights in (False, True):
             before = 0
             for T in sorted(torch.randint(1, 70000, (400,), generator=g).tolist() + [255, 256, 257, 512, 513, 768, 1024, 1025]):

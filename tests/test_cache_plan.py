@@ -26,10 +26,14 @@ def _plan(exe, B, H, G, W, T):
     return tuple(map(int, subprocess.run([exe, *map(str, (B, H, G, W, T))], check=True, capture_output=True, text=True).stdout.split()))
 
 
-def test_decode_steps_read_their_operands_straight_from_memory_and_prompts_share_them(plan):
-    for G, W in [(1, 1), (8, 1), (16, 1), (4, 8), (8, 12)]:
-        assert _plan(plan, 1, 8, G, W, 8192)[0] == 16
-    for G, W in [(1, 97), (4, 512), (7, 203)]:
+def test_tiles_follow_the_rows_and_the_work(plan):
+    for G, W in [(1, 1), (8, 1), (16, 1)]:
+        assert _plan(plan, 1, 8, G, W, 8192)[0] == _plan(plan, 64, 8, G, W, 65536)[0] == 16
+    for G, W in [(20, 1), (4, 8), (8, 12)]:
+        assert _plan(plan, 1, 8, G, W, 8192)[0] == 16 and _plan(plan, 64, 8, G, W, 512)[0] == 16
+        assert _plan(plan, 16, 8, G, W, 8192)[0] == 32
+    assert _plan(plan, 1, 1, 97, 1, 64)[0] == _plan(plan, 16, 8, 8, 16, 8192)[0] == 32
+    for G, W in [(1, 129), (4, 512), (7, 203)]:
         assert _plan(plan, 1, 8, G, W, 8192)[0] == 256
 
 
@@ -37,5 +41,5 @@ def test_few_cells_split_the_tokens(plan):
     assert _plan(plan, 1, 1, 4, 1, 131072)[1] == 256          # a block per compute unit
     assert _plan(plan, 1, 8, 4, 1, 4096)[1] == 16             # 256 tokens a block at least
     assert _plan(plan, 1, 8, 4, 1, 256)[1] == 1
-    assert _plan(plan, 4, 4, 4, 24, 30000)[1] == 5            # 192 blocks would leave a quarter of them idle
+    assert _plan(plan, 4, 4, 24, 24, 30000)[1] == 5           # 96 cells: 192 blocks would leave a quarter of them idle
     assert _plan(plan, 64, 8, 8, 1, 12288)[1] == 1

@@ -2,10 +2,12 @@
 pools and batches beyond 4 GiB, results that the binding allocates on another stream, weights that are no numbers."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 import cache_inputs as inputs
+import cache_reference as ref
 from test_gpu_cache_attend import _check
 from test_gpu_cache_evict import _acc, _run
 
@@ -113,3 +115,29 @@ def test_weights_that_are_not_finite():
         again = torch.empty_like(idx)
         kvp.kvp_cache_evict(c, weights, 60, e, sink=3, recent=20, keep_idx=again)
         assert torch.equal(again, idx)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("B,W,G,n", [(24, 5, 4, 16500), (12, 8, 8, 16500), (40, 3, 11, 7000), (3, 16, 8, 1500)])
+def test_tiles_of_32_rows(fmt, B, W, G, n):
+    # work enough for tiles of 32 rows, most sequences short; two whole ones against the definition, through the cache of the batch
+    import paper_2512_14946_amd as kvp
+    few = inputs.filled_cache(kvp, [n, 77], -(-n // 64), 1, 64, fmt, W, DEV)
+    rows = torch.arange(B, device=DEV) % 2
+    c = kvp.KVCache(few.k_codes, few.v_codes, few.k_scales, few.v_scales, few.block_table[rows].contiguous(), few.lens[rows].contiguous(), fmt)
+    q = inputs.rows((2, W, G, 128), 3, False).to(DEV)
+    acc = torch.zeros(B, 1, n, device=DEV)
+    many = kvp.kvp_cache_attend(q[rows].contiguous(), c, max_len=n, acc_out=acc)
+    model = ref.Cache(few, fmt)
+    want, drawn, mag, vmax, size = ref.attend(model, q.float().cpu(), None, True, 1 / math.sqrt(128))
+    tol = ref.out_tolerance(want, mag, vmax, size, model.lens)
+    err = np.abs(many[:2].double().cpu().numpy() - want)
+    assert np.all(err <= tol), (err / tol).max()
+    assert torch.equal(many[2:4], many[:2]) if B > 3 else torch.equal(many[2], many[0])
+    a = acc.double().cpu().numpy()
+    for b in range(2):
+        m = int(model.lens[b])
+        t = ref.drawn_tolerance(drawn[b:b + 1, :, :m], np.zeros((1, 1, m)), size[b:b + 1])[0]
+        e = np.abs(a[b, :, :m] - drawn[b, :, :m])
+        assert np.all(e <= t), (e / t).max()
+        assert np.all(a[b, :, m:] == 0.0) and np.array_equal(a[b], a[b + 2 if b + 2 < B else b])

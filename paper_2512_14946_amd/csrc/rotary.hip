@@ -9,11 +9,13 @@
 // their heads, and one sine and cosine per (token, pair) go to LDS once and serve every head: 4 x 8192 x 8 rows 23.7 us, 5.7 TB/s.  With a position
 // per head a lane forms those of its own eight pairs: 80 x 4916 x 8 rows 273 us, 6.0 TB/s (580 us by way of
 // LDS with a library sincospi of 25 instructions).  Pairs that do not fall on such pieces (half layout, rotary_dim not a multiple of 16) take a
-// kernel with a wave per row.
+// kernel whose lanes find the other channel in LDS: 63 x 1944 x 8 rows, 2 of 128 channels, 85 us, 5.9 TB/s (a wave per row, two bytes a
+// lane: 276); 34 channels 107.
 
 #include <math.h>
 
 #include "kvp_common.h"
+#include "quant_device.h"
 
 namespace kvp {
 namespace {
@@ -185,24 +187,60 @@ __global__ __launch_bounds__(kThreads) void rotary_rows_kernel(const RotaryArgs 
   }
 }
 
-// Half layout with any even rotary_dim: a wave per row, lane i turns pair i and copies channels behind the pairs.  Both
-// channels of a pair belong to one lane, so a row may be turned in place.
+// Half layout with any even rotary_dim: 16 lanes share a row, a 16-byte piece each; the other channel of a pair lies anywhere in the row and
+// comes by way of LDS.  Both lanes of a pair work out its turn.  A row may be turned in place: it is in LDS before any of it is written.
+constexpr int kRowPitch = kHeadDim + 8;
 __global__ __launch_bounds__(kThreads) void rotary_any_kernel(const RotaryArgs a) {
-  const uint32_t l = blockIdx.y, row = blockIdx.x * (kThreads / kWave) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= a.T * a.H) return;
-  const uint32_t t = a.div_h.quot(row), h = row - t * a.H;
-  const uint16_t* src = a.x + static_cast<int64_t>(l) * a.x_sl + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh;
-  uint16_t* dst = a.out + static_cast<int64_t>(l) * a.o_sl + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh;
-  const int32_t pos = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
-  if (lane < a.pairs) {
-    float p = __uint_as_float(static_cast<uint32_t>(src[lane]) << 16), q = __uint_as_float(static_cast<uint32_t>(src[lane + a.pairs]) << 16);
-    rotate(p, q, turn_of(a, pos, a.freq[lane] * kTurn));
-    const uint32_t w = pack_bf16x2(p, q);
-    dst[lane] = static_cast<uint16_t>(w);
-    dst[lane + a.pairs] = static_cast<uint16_t>(w >> 16);
+  __shared__ __attribute__((aligned(16))) uint16_t row_s[kRows * kThreads / 16][kRowPitch];
+  const uint32_t l = blockIdx.y, j = threadIdx.x & 15, n_rows = a.T * a.H, row0 = blockIdx.x * (kRows * kThreads / 16) + (threadIdx.x >> 4);
+  const bool turns = 8 * j < 2 * a.pairs, works = turns || a.copy;
+  double f[8];   // of this lane's channels, in turns
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    const uint32_t c = 8 * j + e;
+    f[e] = c < 2 * a.pairs ? a.freq[c < a.pairs ? c : c - a.pairs] * kTurn : 0.0;
   }
-  if (a.copy)
-    for (uint32_t c = 2 * a.pairs + lane; c < kHeadDim; c += kWave) dst[c] = src[c];
+  uint4 v[kRows];
+  int32_t pos[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const uint32_t row = row0 + k * (kThreads / 16), t = a.div_h.quot(row), h = row - t * a.H;
+    if (row >= n_rows || !works) continue;
+    if (turns) pos[k] = a.pos[static_cast<int64_t>(l) * a.p_sl + static_cast<int64_t>(t) * a.p_st + static_cast<int64_t>(h) * a.p_sh];
+    v[k] = load_stream16(a.x + static_cast<int64_t>(l) * a.x_sl + static_cast<int64_t>(t) * a.x_st + static_cast<int64_t>(h) * a.x_sh + 8 * j);
+  }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k)
+    if (turns && row0 + k * (kThreads / 16) < n_rows) *reinterpret_cast<uint4*>(&row_s[k * (kThreads / 16) + (threadIdx.x >> 4)][8 * j]) = v[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const uint32_t row = row0 + k * (kThreads / 16), t = a.div_h.quot(row), h = row - t * a.H;
+    if (row >= n_rows || !works) continue;
+    if (turns) {
+      const uint16_t* x = row_s[k * (kThreads / 16) + (threadIdx.x >> 4)];
+      uint32_t* w = reinterpret_cast<uint32_t*>(&v[k]);
+      float y[8];
+      unpack_bf16x8(v[k], y);
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {
+        const uint32_t c = 8 * j + e;
+        if (c >= 2 * a.pairs) continue;
+        const float2 cs = turn_of(a, pos[k], f[e]);
+        float p = y[e], q = __uint_as_float(static_cast<uint32_t>(x[c < a.pairs ? c + a.pairs : c - a.pairs]) << 16);
+        if (c < a.pairs) {
+          rotate(p, q, cs);
+        } else {
+          rotate(q, p, cs);
+        }
+        y[e] = p;
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (8 * j + 2 * i < 2 * a.pairs) w[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
+    }
+    store_stream16(a.out + static_cast<int64_t>(l) * a.o_sl + static_cast<int64_t>(t) * a.o_st + static_cast<int64_t>(h) * a.o_sh + 8 * j, v[k]);
+  }
 }
 
 }  // namespace
@@ -242,9 +280,9 @@ extern "C" int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int3
   const hipStream_t st = as_stream(stream);
   const unsigned layers = static_cast<unsigned>(x->L);
   if (layout == KVP_ROTARY_HALF && rotary_dim % 16) {
-    const int64_t rows = x->T * x->H;
-    if (!fits_grid(ceil_div(rows, kThreads / kWave), kThreads)) return KVP_ERR_SHAPE;
-    rotary_any_kernel<<<dim3(static_cast<unsigned>(ceil_div(rows, kThreads / kWave)), layers), kThreads, 0, st>>>(a);
+    const int64_t blocks = ceil_div(x->T * x->H, kRows * kThreads / 16);
+    if (!fits_grid(blocks, kThreads)) return KVP_ERR_SHAPE;
+    rotary_any_kernel<<<dim3(static_cast<unsigned>(blocks), layers), kThreads, 0, st>>>(a);
     return launch_status();
   }
   if (pos_stride_h != 0) {

@@ -223,7 +223,7 @@ def test_launches_beyond_what_a_grid_takes_are_refused():
     assert evict(src=c, dst=cache(block_table=1 << 21, **big), budget=1 << 24, stride=1 << 24, ws_bytes=1 << 62) == SHAPE
     wide = cache(B=1 << 22, num_blocks=1, max_blocks=1, table_stride=1)
     assert attend(q=view(L=1 << 22, H=8), out=view(L=1 << 22, H=8, ptr=1 << 30), c=wide, ws_bytes=1 << 62) == SHAPE
-    assert rotary(x=view(T=1 << 24, H=8), rd=8) == SHAPE
+    assert rotary(x=view(T=1 << 27, H=8), rd=8) == SHAPE
 
 
 def test_a_workspace_serves_every_smaller_bound():

@@ -8,8 +8,8 @@
 // that the lane's operand of O^T = V^T P^T takes: the probabilities never leave the lane, and its operand of V^T is 16 consecutive
 // bytes of a channel, which is why values are stored channel-major.  Codes become halves in registers (exact); the page
 // scale of the keys multiplies the logits, that of the values the probabilities (relative to the largest one so far, so that
-// halves hold them).  Logits are kept in base 2.  The reference that exponentials are taken against follows the maximum
-// lazily: it moves only when a logit exceeds it by 2^8, which P in halves and the sums in fp32 bear.
+// halves hold them).  Logits are kept in base 2.  The reference that exponentials are taken against is set 2^10 below the maximum and follows it
+// lazily: it moves only when a probability times its page's share exceeds 2^15.5, which halves and the sums in fp32 bear.
 //
 // This file: up to 128 query rows per (sequence, head) in tiles of 16 or 32, a decode step above all, bound by HBM.  A block's waves take a quarter
 // of its chunk each, with the loads of the next 64 tokens always in flight; partial results of chunks are joined by a second kernel.
@@ -34,6 +34,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr int kWaves = kAttendWaves;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeptFloats = 4096;           // logits that a wave keeps in LDS: 4 tiles of 16 rows, 8 of 8
+constexpr float kMostLog = 15.5f;           // log2 of the most that a probability times its page's share may be: halves end at 2^16
 constexpr int kOutPitch = 132;              // floats per row of partial outputs in LDS
 constexpr uint32_t kSlice = 4 * kThreads;   // tokens of a block that sums weights from logits
 
@@ -212,15 +213,18 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       }
       ++n_kept;
     }
+    // Probabilities times the page's share of the reference scale: the share goes into the exponent, and the sum of the tile is divided by it.
+    // A share below 2^-60 leaves nothing of a half either way, and a page of zeros has none: both count as 2^-60.
+    float log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f);
     float top[R];
-    bool moves = vs_now > kValueSlack * vref;
+    bool moves = false;
 #pragma unroll
     for (int u = 0; u < R; ++u) {
       top[u] = s[u][0][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top[u] = fmaxf(top[u], s[u][i >> 2][i & 3]);
       top[u] *= f[u];                        // f > 0
-      moves = moves || top[u] > ref[u] + kSlack;
+      moves = moves || log_share + fmaxf(top[u] - ref[u], 0.0f) > kMostLog;   // a share alone too: what is masked may lie in a page of any scale
     }
     if (__builtin_amdgcn_ballot_w64(moves)) {   // wave-uniform
       float v_new = fmaxf(vref, vs_now);
@@ -228,8 +232,9 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       v_new = fmaxf(v_new, __shfl_xor(v_new, 32));
 #pragma unroll
       for (int u = 0; u < R; ++u) {
-        float ref_new = fmaxf(ref[u], fmaxf(top[u], __shfl_xor(top[u], 16)));
-        ref_new = fmaxf(ref_new, __shfl_xor(ref_new, 32));
+        float most = fmaxf(top[u], __shfl_xor(top[u], 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float ref_new = fmaxf(ref[u], most - kBelow);
         const float down = __builtin_amdgcn_exp2f(ref[u] - ref_new), down_o = down * (vref / v_new);
         sum[u] *= down;
 #pragma unroll
@@ -238,10 +243,9 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       }
       vref = v_new;
       inv_vref = 1.0f / v_new;
+      log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f);
     }
-    // Probabilities times the page's share of the reference scale: the share goes into the exponent, and the sum of the tile is divided by it.
-    // A share below 2^-60 leaves nothing of a half either way, and a page of zeros has none: both count as 2^-60.
-    const float log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f), per_share = __builtin_amdgcn_exp2f(-log_share);
+    const float per_share = __builtin_amdgcn_exp2f(-log_share);
     half8_t pf[R][2];
 #pragma unroll
     for (int u = 0; u < R; ++u) {
@@ -301,13 +305,18 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
     float m = ref_s[0][orow];
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) m = fmaxf(m, ref_s[i][orow]);
-    float z = 0.0f, y[8] = {};
+    float e[kWaves], z = 0.0f, y[8] = {};
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      const float e = __builtin_amdgcn_exp2f(ref_s[i][orow] - m), ev = e * val_s[i];
-      z = fmaf(sum_s[i][orow], e, z);
+      e[i] = __builtin_amdgcn_exp2f(ref_s[i][orow] - m);
+      z = fmaf(sum_s[i][orow], e[i], z);
+    }
+    const float inv = z > 0.0f ? 1.0f / z : 0.0f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = fmaf(shared_s[i * kOutFloats + orow * kOutPitch + ch + j], ev, y[j]);
+    for (int i = 0; i < kWaves; ++i) {
+      const float part = e[i] * inv, scale = val_s[i];   // divided by the sum first, then times the scale: neither leaves binary32's range
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = fmaf(shared_s[i * kOutFloats + orow * kOutPitch + ch + j] * part, scale, y[j]);
     }
     const int64_t at = (static_cast<int64_t>(cell) * a.chunks + chunk) * kRows + orow;
     const uint32_t row = r.tile * kRows + orow, w = a.div_g.quot(row);
@@ -320,11 +329,9 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       continue;
     }
     if (row >= a.M || static_cast<int32_t>(w) >= r.m) continue;
-    const float inv = z > 0.0f ? 1.0f / z : 0.0f;
     if (a.row_bias && ch == 0) a.row_bias[static_cast<int64_t>(cell) * kRows + orow] = bias_of(m, z);
     uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw + static_cast<int64_t>(r.h * a.G + (row - w * a.G)) * a.o_sh + ch;
-    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv),
-                                                pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
   }
 }
 
@@ -370,7 +377,8 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
     for (uint32_t i = group; i < n; i += 8) {
-      const float f = __builtin_amdgcn_exp2f(st[static_cast<int64_t>(i) * a.tile_rows].x - stat.x);
+      const float2 s = st[static_cast<int64_t>(i) * a.tile_rows];
+      const float f = __builtin_amdgcn_exp2f(s.x - stat.x) * (s.y * inv);   // the chunk's part of the row's weight
       const float4 u = po[static_cast<int64_t>(i) * a.tile_rows * (kHeadDim / 4)];
       y.x = fmaf(u.x, f, y.x); y.y = fmaf(u.y, f, y.y); y.z = fmaf(u.z, f, y.z); y.w = fmaf(u.w, f, y.w);
     }
@@ -384,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void cache_join_kernel(const AttendArgs a
     }
     uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw +
                     static_cast<int64_t>(r.h * a.G + (row - w * a.G)) * a.o_sh + ch * 4;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
     return;
   }
   // one row tile per (sequence, head) here: a cell is a (sequence, head)

@@ -30,7 +30,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeyPitch = 65, kValuePitch = 66;   // 16-byte slots from one operand to the next
 constexpr float kLeastLog = -100.0f;         // log2 of value scales: one below counts as this one's fraction
-constexpr float kMostPart = 16384.0f;        // most that eight probabilities, as halves, may sum to before the reference moves
+constexpr float kMostPart = 60000.0f;        // most that eight probabilities, as halves, may sum to before the reference moves; just after it did, 2^13
 constexpr int kBuffers = 4;       // tiles in LDS: being multiplied, next, being staged, and one of slack
 static_assert(kManyRows == 32 * kWaves, "a wave owns 32 rows");
 
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
         float top = -INFINITY;
 #pragma unroll
         for (int k = 0; k < 32; ++k) top = fmaxf(top, s[k >> 4][k & 15] * f[k >> 3]);
-        const float ref_new = fmaxf(ref, fmaxf(top, __shfl_xor(top, 32)));
+        const float ref_new = fmaxf(ref, fmaxf(top, __shfl_xor(top, 32)) - kBelow);
         const float v_new = fmaxf(vref, fmaxf(fmaxf(v_u[0], v_u[1]), fmaxf(v_u[2], v_u[3])));
         const float down = __builtin_amdgcn_exp2f(ref - ref_new), down_o = down * __builtin_amdgcn_exp2f(vref - v_new);
         sum *= down;
@@ -297,7 +297,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
     if (!late) block_step();
   }
 
-  const float z = sum + __shfl_xor(sum, 32), scale = __builtin_amdgcn_exp2f(vref);
+  const float z = sum + __shfl_xor(sum, 32), inv = z > 0.0f ? 1.0f / z : 0.0f, scale = __builtin_amdgcn_exp2f(vref);
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[c][i] = o[c][i] * inv * scale;   // in this order nothing leaves binary32's range
   if (!valid) return;
   const uint32_t in_tile = wave * 32 + col;
   if (a.chunks > 1) {
@@ -308,18 +312,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_rows_kernel(const AttendAr
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<float4*>(a.part_out + at * kHeadDim + 32 * c + 8 * i + 4 * hb) =
-            make_float4(o[c][4 * i] * scale, o[c][4 * i + 1] * scale, o[c][4 * i + 2] * scale, o[c][4 * i + 3] * scale);
+            make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
     return;
   }
   if (a.row_bias && hb == 0) a.row_bias[static_cast<int64_t>(cell) * a.tile_rows + in_tile] = bias_of(ref, z);
-  const float inv = z > 0.0f ? scale / z : 0.0f;
   uint16_t* dst = a.out + static_cast<int64_t>(r.b) * a.o_sb + static_cast<int64_t>(w) * a.o_sw + static_cast<int64_t>(head) * a.o_sh;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<uint2*>(dst + 32 * c + 8 * i + 4 * hb) =
-          make_uint2(pack_bf16x2(o[c][4 * i] * inv, o[c][4 * i + 1] * inv), pack_bf16x2(o[c][4 * i + 2] * inv, o[c][4 * i + 3] * inv));
+          make_uint2(pack_bf16x2(o[c][4 * i], o[c][4 * i + 1]), pack_bf16x2(o[c][4 * i + 2], o[c][4 * i + 3]));
 }
 
 // What every token drew from all rows: drawn_t = sum over rows 2^(s_rt - bias_r).  A wave owns 32 tokens of a (sequence, head), their keys as

@@ -409,7 +409,7 @@ def _check(rc: int, what: str):
 def _torch_stream(stream, device):
     if stream is None:
         return torch.cuda.current_stream(device)
-    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
 
 
 def _workspace(ws, nbytes: int, device, stream=None):

@@ -2,9 +2,13 @@
 
 Argument marshalling only.  torch supplies device memory and the current HIP stream; every
 kernel launch happens inside the C library.
+
+`stream` is a torch.cuda.Stream or a raw handle, None for torch's current one.  What a call allocates, results and temporaries,
+belongs to that stream, as if allocated under torch.cuda.stream(stream).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -412,18 +416,22 @@ def _torch_stream(stream, device):
     return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _on(stream, device):
+    """Where a call's results and temporaries are allocated (and cleared): on the stream that the call runs on.  torch's allocator
+    hands out blocks that kernels of the current stream still use, which only later work of that stream waits for."""
+    return _HERE if stream is None else torch.cuda.stream(_torch_stream(stream, device))
+
+
 def _workspace(ws, nbytes: int, device, stream=None):
-    """(tensor kept alive by the caller, pointer, bytes).  A workspace allocated here is a temporary: when the
-    call runs on a stream other than torch's current one, the allocator is told so that it does not hand the
-    memory out again while the kernels still use it."""
+    """(tensor kept alive by the caller, pointer, bytes).  A workspace allocated here is a temporary of the call's stream."""
     if ws is None:
         if nbytes == 0:
             return None, None, 0
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream is not None:
-            s = _torch_stream(stream, device)
-            if s != torch.cuda.current_stream(device):
-                ws.record_stream(s)
+        with _on(stream, device):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -435,9 +443,10 @@ def kvp_strerror(code: int) -> str:
 
 def kvp_selftest_reciprocal(stream=None) -> int:
     """Operands (of 2^23 x 121) for which the corrected hardware reciprocal differs from the IEEE quotient."""
-    out = torch.zeros(1, dtype=torch.int64, device="cuda")
-    _check(_lib.kvp_selftest_reciprocal(out.data_ptr(), _stream(stream)), "kvp_selftest_reciprocal")
-    return int(out.item())
+    with _on(stream, torch.device("cuda", torch.cuda.current_device())):
+        out = torch.zeros(1, dtype=torch.int64, device="cuda")
+        _check(_lib.kvp_selftest_reciprocal(out.data_ptr(), _stream(stream)), "kvp_selftest_reciprocal")
+        return int(out.item())
 
 
 def kvp_version() -> int:
@@ -512,7 +521,8 @@ def kvp_score_tokens(q_win: torch.Tensor, k: torch.Tensor, scores: torch.Tensor 
     L, T, Hkv, _ = k.shape
     _, W, Hq, _ = q_win.shape
     if scores is None:
-        scores = torch.empty(L, Hkv, T, dtype=torch.float32, device=k.device)
+        with _on(stream, k.device):
+            scores = torch.empty(L, Hkv, T, dtype=torch.float32, device=k.device)
     if scores.dtype != torch.float32 or not scores.is_contiguous() or tuple(scores.shape) != (L, Hkv, T):
         raise ValueError("scores must be contiguous float32 [L][Hkv][T]")
     ws, wp, wb = _workspace(ws, kvp_score_workspace_bytes(L, Hkv, Hq, W, T), k.device, stream)
@@ -552,7 +562,8 @@ def kvp_score_keys(k: torch.Tensor, method: int, scores: torch.Tensor | None = N
     _need_cuda(k, scores, ws)
     L, T, H, _ = k.shape
     if scores is None:
-        scores = torch.empty(L, H, T, dtype=torch.float32, device=k.device)
+        with _on(stream, k.device):
+            scores = torch.empty(L, H, T, dtype=torch.float32, device=k.device)
     if scores.dtype != torch.float32 or not scores.is_contiguous() or tuple(scores.shape) != (L, H, T):
         raise ValueError("scores must be contiguous float32 [L][H][T]")
     ws, wp, wb = _workspace(ws, kvp_score_keys_workspace_bytes(L, H, T, method), k.device, stream)
@@ -575,7 +586,8 @@ def kvp_select_topk(scores: torch.Tensor, k: int, idx_out: torch.Tensor | None =
     n_rows, T = scores.shape
     row_stride = scores.stride(0) if n_rows > 1 else T
     if idx_out is None:
-        idx_out = torch.empty(n_rows, k, dtype=torch.int32, device=scores.device)
+        with _on(stream, scores.device):
+            idx_out = torch.empty(n_rows, k, dtype=torch.int32, device=scores.device)
     if idx_out.dtype != torch.int32 or not idx_out.is_contiguous() or tuple(idx_out.shape) != (n_rows, k):
         raise ValueError("idx_out must be contiguous int32 [n_rows][k]")
     ws, wp, wb = _workspace(ws, kvp_select_workspace_bytes(n_rows, T, k), scores.device, stream)
@@ -592,7 +604,8 @@ def kvp_smooth_scores(scores: torch.Tensor, window: int, kernel: int, mode: str 
         raise ValueError("scores must be float32 [n_rows][T] with contiguous rows")
     n_rows, T = scores.shape
     if out is None:
-        out = torch.empty(n_rows, T, dtype=torch.float32, device=scores.device)
+        with _on(stream, scores.device):
+            out = torch.empty(n_rows, T, dtype=torch.float32, device=scores.device)
     if out.dtype != torch.float32 or tuple(out.shape) != (n_rows, T) or (T > 1 and out.stride(1) != 1):
         raise ValueError("out must be float32 [n_rows][T] with contiguous rows")
     _check(_lib.kvp_smooth_scores(scores.data_ptr(), n_rows, T, scores.stride(0) if n_rows > 1 else T, window, kernel,
@@ -618,9 +631,11 @@ def kvp_eval_configs(q_win: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cfgs
     _, W, Hq, _ = q_win.shape
     arr = (_Config * max(n, 1))(*[_Config(int(b), int(g), int(kk)) for b, g, kk in cfgs])
     if loss is None:
-        loss = torch.empty(n, dtype=torch.float32, device=k.device)
+        with _on(stream, k.device):
+            loss = torch.empty(n, dtype=torch.float32, device=k.device)
     if want_partial and partial is None:
-        partial = torch.empty(L, n, 2, dtype=torch.float32, device=k.device)
+        with _on(stream, k.device):
+            partial = torch.empty(L, n, 2, dtype=torch.float32, device=k.device)
     ws, wp, wb = _workspace(ws, kvp_eval_workspace_bytes(L, Hkv, Hq, W, T, n), k.device, stream)
     qv, kv, vv = _view(q_win), _view(k), _view(v)
     pp = partial.data_ptr() if partial is not None else None
@@ -710,10 +725,10 @@ def kvp_cache_attend(q: torch.Tensor, cache: KVCache, out: torch.Tensor | None =
     that every token drew.  max_len: an upper bound of lens, 0 for the capacity.  Rows behind q_lens[b] are not written."""
     cs = _cache(cache)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        if q_lens is not None:      # rows that no call writes, cleared on the stream that the call runs on
-            with torch.cuda.stream(_torch_stream(stream, q.device)):
-                out.zero_()
+        with _on(stream, q.device):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            if q_lens is not None:
+                out.zero_()      # rows that the call does not write
     _one_device(cache.k_codes, q, out, q_lens, acc_in, acc_out, ws)
     qv, ov = _view(q), _view(out)
     cap = cs.max_blocks * cs.bs
@@ -790,7 +805,8 @@ def kvp_rotary(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, out
     if layout not in _ROTARY_LAYOUTS:
         raise ValueError('layout must be "half" or "interleaved"')
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        with _on(stream, x.device):
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
     _one_device(x, out, positions, freq)
     xv, ov = _view(x), _view(out)
     if positions.dtype != torch.int32:

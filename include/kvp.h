@@ -312,7 +312,8 @@ int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, const kvp_v
  * scale is rounded to 11 bits (2^-11 relative) or to 2^-35 of the row's largest probability times the largest value scale,
  * 2^-100 at least, whichever is coarser.  Finite q and cache contents, finite scale: a row that does not see a token is still
  * spoiled by a value of it that is not finite.
- * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256) below 2^23, B * H * max_len / 128 below 2^24. */
+ * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256), for W * G up to 128 B * H * ceil(W * G / 16), below 2^23 - 7;
+ * with acc_out B * H * ceil(max_len / 128) below 2^24. */
 int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,
                          const kvp_view* out, const float* acc_in, float* acc_out, int64_t acc_stride, int64_t max_len,
                          void* ws, size_t ws_bytes, void* stream);

@@ -36,7 +36,8 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kKeptFloats = 4096;           // logits that a wave keeps in LDS: 4 tiles of 16 rows, 8 of 8
 constexpr float kMostLog = 15.5f;           // log2 of the most that a probability times its page's share may be: halves end at 2^16
 constexpr int kOutPitch = 132;              // floats per row of partial outputs in LDS
-constexpr uint32_t kSlice = 4 * kThreads;   // tokens of a block that sums weights from logits
+constexpr uint32_t kSlice = kJoinTokens;
+static_assert(kSlice == 4 * kThreads, "16 threads a tile of 64 tokens");
 
 // One query row as operands of the four channel steps: halves of q / 2^e with the sign of the softmax scale, and the positive factor that turns
 // their products with codes into base-2 logits.
@@ -464,10 +465,8 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   if (acc_out && acc_stride < max_len) return KVP_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(q_lens) | reinterpret_cast<uintptr_t>(acc_in) | reinterpret_cast<uintptr_t>(acc_out)) & 3u) return KVP_ERR_ALIGN;
   const AttendPlan p = make_attend_plan(cache->B, cache->H, q->H, W, max_len, acc_out != nullptr);
-  // blocks of both passes over the keys (512 threads at most), of the join and of the weights
-  if (!fits_grid(p.cells * p.chunks, 512) || !fits_grid(p.cells * (p.tile_rows + ceil_div(max_len, kSlice)), kThreads) ||
-      !fits_grid(cache->B * cache->H * ceil_div(max_len, kSumTokens), kThreads))
-    return KVP_ERR_SHAPE;
+  const AttendBlocks blocks = attend_blocks(p, cache->B * cache->H, W * G, max_len, acc_out != nullptr);
+  if (!attend_fits(blocks)) return KVP_ERR_SHAPE;
   if (p.bytes != 0 && (!ws || ws_bytes < p.bytes || !aligned16(ws))) return KVP_ERR_WORKSPACE;
   if (out->ptr == q->ptr) return KVP_ERR_SHAPE;   // several blocks, and the weights' pass, read a query row
   AttendArgs a{};
@@ -489,7 +488,7 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   a.div_h = FastDiv(a.c.H);
   a.div_g = FastDiv(a.G);
   a.blocks = static_cast<uint32_t>(p.cells * p.chunks);
-  a.per_xcd = (a.blocks + 7) / 8;
+  a.per_xcd = static_cast<uint32_t>(blocks.attend / 8);
   a.div_bh = FastDiv(a.chunks * a.row_tiles);
   a.scale2 = scale * kLog2e;
   a.causal = causal;
@@ -513,10 +512,9 @@ extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, c
   else
     few_rows_launch<KVP_CACHE_E4M3>(a, grid, keep, p.tile_rows, st);
   const uint32_t join_rows = std::min(a.M, a.tile_rows), slices = static_cast<uint32_t>(ceil_div(max_len, kSlice));
-  const int64_t n_join = p.chunks > 1 ? p.cells * join_rows : 0, n_sum = p.logit_bytes ? p.cells * slices : 0;
-  if (n_join + n_sum > 0)
-    cache_join_kernel<<<dim3(static_cast<unsigned>(n_join + n_sum)), kThreads, 0, st>>>(a, static_cast<uint32_t>(n_join), join_rows, FastDiv(join_rows),
-                                                                                       slices, FastDiv(slices));
-  if (acc_out && !p.logit_bytes) weights_rows_launch(a, cache->format, st);
+  if (blocks.join_rows + blocks.join_sums > 0)
+    cache_join_kernel<<<dim3(static_cast<unsigned>(blocks.join_rows + blocks.join_sums)), kThreads, 0, st>>>(
+        a, static_cast<uint32_t>(blocks.join_rows), join_rows, FastDiv(join_rows), slices, FastDiv(slices));
+  if (blocks.sums > 0) weights_rows_launch(a, cache->format, st);
   return launch_status();
 }

@@ -16,6 +16,7 @@ constexpr int kFewRows = 128;     // rows up to which those blocks are taken
 constexpr int kManyRows = 256;    // ... of a block that shares its tiles by way of LDS
 constexpr int kAttendWaves = 4;
 constexpr int kSumTokens = 128;   // tokens of a block that sums the weights of many rows
+constexpr int kJoinTokens = 1024; // ... of a block of the joining kernel that sums weights from logits
 constexpr int kUnits = 256;       // CUs
 
 struct AttendPlan {
@@ -94,6 +95,25 @@ inline AttendPlan make_attend_plan(int64_t B, int64_t H, int64_t Hq, int64_t W, 
   if (rows == 2 * kTileRows && M <= 96)
     p.bytes = std::max(p.bytes, make_attend_plan_of(kTileRows, B, H, M, wide_tiles_from(B * H, M) - 1, weights).bytes);
   return p;
+}
+
+// Blocks of the launches that a plan takes (0: none): the attention's (512 threads at most), the joining kernel's (rows of chunks, and weights
+// from kept logits; 256) and those that sum the weights of many rows (256).
+struct AttendBlocks {
+  int64_t attend, join_rows, join_sums, sums;
+};
+
+inline AttendBlocks attend_blocks(const AttendPlan& p, int64_t n_bh, int64_t M, int64_t T, bool weights) {
+  AttendBlocks n{};
+  n.attend = ceil_div(p.cells * p.chunks, 8) * 8;   // a whole number of blocks for each of the 8 XCDs
+  if (p.chunks > 1) n.join_rows = p.cells * std::min(M, p.tile_rows);
+  if (p.logit_bytes) n.join_sums = p.cells * ceil_div(T, kJoinTokens);
+  if (weights && !p.logit_bytes) n.sums = n_bh * ceil_div(T, kSumTokens);
+  return n;
+}
+
+inline bool attend_fits(const AttendBlocks& n) {
+  return fits_grid(n.attend, 512) && fits_grid(n.join_rows + n.join_sums, 256) && fits_grid(n.sums, 256);
 }
 
 }  // namespace kvp

@@ -17,9 +17,6 @@ inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline int32_t launch_status() { return hipGetLastError() == hipSuccess ? KVP_OK : KVP_ERR_LAUNCH; }
 
-// A launch takes fewer than 2^32 threads.
-inline bool fits_grid(int64_t blocks, int64_t threads) { return blocks < (1ll << 32) / threads; }
-
 // Division of a non-negative n < 2^31 by a divisor fixed at launch: multiply-high and shift.
 struct FastDiv {
   uint32_t mul, shift, d;

@@ -1,0 +1,47 @@
+"""What kvp_cache_attend accepts and refuses by size: its launches (csrc/cache_attend_plan.h) walked over the limits of the header, and shapes on
+either side through the C ABI (whose pointers are never followed: what is accepted ends at the missing workspace)."""
+import os
+import subprocess
+
+import pytest
+
+import paper_2512_14946_amd as kvp
+from test_cache_abi import SHAPE, WORKSPACE, attend, cache, view
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def limits(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("cache_limits") / "cache_limits")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2512_14946_amd", "csrc"), "-o", exe,
+                    os.path.join(ROOT, "tests", "cache_limits.cpp")], check=True)
+    return exe
+
+
+def test_every_size_within_the_limits_fits_its_launches(limits):
+    out = subprocess.run([limits], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
+    assert int(out.stdout) > 100_000
+
+
+@pytest.mark.parametrize("B,W,T", [(8, 32768, 32768), (32, 8192, 8192), (2, 131072, 131072), (16, 16384, 16384)])
+def test_large_prompts_take_one_launch(limits, B, W, T):
+    H, G = 8, 8
+    n = list(map(int, subprocess.run([limits, *map(str, (B, H, G, W, T, 0))], check=True, capture_output=True, text=True).stdout.split()))
+    assert n == [B * H * -(-W * G // 256), 0, 0, 0, 1]
+    assert kvp.kvp_cache_attend_workspace_bytes(B, H, G * H, W, T, False) == 0
+
+
+def _sized(B, H, G, W, T, **kw):
+    c = cache(B=B, H=H, bs=16, max_blocks=-(-T // 16), table_stride=-(-T // 16), num_blocks=1)
+    q = view(L=B, T=W, H=G * H)
+    return attend(q=q, out=view(L=B, T=W, H=G * H, ptr=1 << 50), c=c, acc_out=4096, stride=T + 16, ws=None, **kw)
+
+
+@pytest.mark.parametrize("B,H,G,W,T,code", [(8, 8, 8, 32768, 32768, WORKSPACE), (1, 8, 16, 131072, 131072, WORKSPACE), (16, 8, 8, 16384, 16384, WORKSPACE),
+                                            (1 << 20, 7, 1, 200, 128, WORKSPACE), (1 << 20, 8, 1, 200, 128, SHAPE), ((1 << 20) - 1, 8, 1, 200, 128, WORKSPACE),
+                                            (1 << 19, 15, 1, 16, 16, WORKSPACE), (1 << 19, 16, 1, 16, 16, SHAPE), (1 << 19, 8, 1, 17, 16, SHAPE),
+                                            (1 << 13, 8, 1, 130, 32768 - 128, WORKSPACE), (1 << 13, 8, 1, 130, 32768, SHAPE)])
+def test_shapes_on_either_side_of_the_limits(B, H, G, W, T, code):
+    assert _sized(B, H, G, W, T) == code

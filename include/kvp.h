@@ -344,8 +344,9 @@ size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t T, int64_t 
  * h * pos_stride_h; a stride may be 0.  A keep list [L][H][k] (strides H*k, 1, k) gives every kept token of every
  * head its own; keys that were rotated at one position move to another by the difference.  The angle is formed and reduced in
  * double, sine and cosine and the rotation in fp32, the result rounded once to bf16.  out has the shape of x; it may be the same
- * view (in place), or must not overlap it.  rotary_dim even, 2 .. 128; L <= 65535, T and T * H below 2^31 (KVP_ROTARY_HALF with rotary_dim no
- * multiple of 16: 2^30). */
+ * view (in place), or must not overlap it.  rotary_dim even, 2 .. 128; L <= 65535, T * H below 2^31, and
+ * T at most 2^30 - 64 with pos_stride_h = 0, T * H at most 2^31 - 128 otherwise, T * H at most 2^30 - 64 for KVP_ROTARY_HALF with
+ * rotary_dim no multiple of 16. */
 enum { KVP_ROTARY_HALF = 0, KVP_ROTARY_INTERLEAVED = 1 };
 int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int32_t* positions, int64_t pos_stride_l,
                    int64_t pos_stride_t, int64_t pos_stride_h, const double* freq, int32_t rotary_dim, int32_t layout,

@@ -16,13 +16,13 @@
 
 #include "kvp_common.h"
 #include "quant_device.h"
+#include "rotary_plan.h"
 
 namespace kvp {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kRows = 4;                       // rows per lane whose loads are all ahead of the arithmetic
-constexpr int kMaxTokens = 64;                 // tokens of a block
+constexpr int kThreads = kRotaryThreads;
+constexpr int kRows = kRotaryRows;
 
 struct RotaryArgs {
   const uint16_t* x;
@@ -99,7 +99,7 @@ __device__ __forceinline__ bool pieces_of(const RotaryArgs& a, uint32_t j, uint3
 // One position for all heads of a token.
 template <int LAYOUT>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
-  __shared__ float2 cs_s[kMaxTokens * 64];
+  __shared__ float2 cs_s[kRotaryTokens * 64];
   const uint32_t l = blockIdx.y, token0 = blockIdx.x * a.tokens_block, tokens = min(a.tokens_block, a.T - token0);
   for (uint32_t i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
     const uint32_t u = a.div_pairs.quot(i), p = i - u * a.pairs;
@@ -261,6 +261,9 @@ extern "C" int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int3
   if (x->L > 65535 || x->T >= (1ll << 31) || x->H >= (1ll << 31) || x->T * x->H >= (1ll << 31)) return KVP_ERR_SHAPE;
   if (pos_stride_l < 0 || pos_stride_t < 0 || pos_stride_h < 0) return KVP_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(freq) & 7u)) return KVP_ERR_ALIGN;
+  const bool any = layout == KVP_ROTARY_HALF && rotary_dim % 16, per_head = pos_stride_h != 0;
+  const int64_t blocks = rotary_blocks(x->T, x->H, any, per_head);
+  if (!fits_grid(blocks, kThreads)) return KVP_ERR_SHAPE;
   RotaryArgs a{};
   a.x = static_cast<const uint16_t*>(x->ptr);
   a.out = static_cast<uint16_t*>(const_cast<void*>(out->ptr));
@@ -278,27 +281,21 @@ extern "C" int32_t kvp_rotary(const kvp_view* x, const kvp_view* out, const int3
   a.sign = inverse ? -1.0f : 1.0f;
   a.copy = x->ptr != out->ptr;
   const hipStream_t st = as_stream(stream);
-  const unsigned layers = static_cast<unsigned>(x->L);
-  if (layout == KVP_ROTARY_HALF && rotary_dim % 16) {
-    const int64_t blocks = ceil_div(x->T * x->H, kRows * kThreads / 16);
-    if (!fits_grid(blocks, kThreads)) return KVP_ERR_SHAPE;
-    rotary_any_kernel<<<dim3(static_cast<unsigned>(blocks), layers), kThreads, 0, st>>>(a);
-    return launch_status();
-  }
-  if (pos_stride_h != 0) {
-    const dim3 grid(static_cast<unsigned>(ceil_div(x->T * x->H, kRows * kThreads / 8)), layers);
+  const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(x->L));
+  if (any) {
+    rotary_any_kernel<<<grid, kThreads, 0, st>>>(a);
+  } else if (per_head) {
     if (layout == KVP_ROTARY_HALF)
       rotary_rows_kernel<KVP_ROTARY_HALF><<<grid, kThreads, 0, st>>>(a);
     else
       rotary_rows_kernel<KVP_ROTARY_INTERLEAVED><<<grid, kThreads, 0, st>>>(a);
-    return launch_status();
+  } else {
+    a.tokens_block = static_cast<uint32_t>(rotary_tokens_block(x->T, x->H));
+    if (layout == KVP_ROTARY_HALF)
+      rotary_kernel<KVP_ROTARY_HALF><<<grid, kThreads, 0, st>>>(a);
+    else
+      rotary_kernel<KVP_ROTARY_INTERLEAVED><<<grid, kThreads, 0, st>>>(a);
   }
-  a.tokens_block = static_cast<uint32_t>(std::min<int64_t>(kMaxTokens, std::max<int64_t>(1, 64 / x->H)));
-  const dim3 grid(static_cast<unsigned>(ceil_div(a.T, a.tokens_block)), layers);
-  if (layout == KVP_ROTARY_HALF)
-    rotary_kernel<KVP_ROTARY_HALF><<<grid, kThreads, 0, st>>>(a);
-  else
-    rotary_kernel<KVP_ROTARY_INTERLEAVED><<<grid, kThreads, 0, st>>>(a);
   return launch_status();
 }
 

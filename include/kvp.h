@@ -187,7 +187,7 @@ size_t kvp_score_keys_workspace_bytes(int64_t L, int64_t H, int64_t T, int32_t m
  * of n_rows rows of T fp32 scores (row_stride floats apart): the indices of the
  * k largest, equal scores resolved toward the lowest index, written ascending
  * to idx_out [n_rows][k] (device int32).  NaN scores are out of contract.
- * 0 <= k <= T; T < 2^30.  Rows longer than 16384 and up to 2^18 scores are split over several
+ * 0 <= k <= T; T < 2^30; fewer than 2^23 rows, 2^22 of more than 16384 scores.  Rows longer than 16384 and up to 2^18 scores are split over several
  * workgroups and need scratch: kvp_select_workspace_bytes(n_rows, T, k) bytes (16 bytes for two
  * pivots and a flag per row, two counts per 16384-score span, 64 KiB of candidate slots per
  * row), 16-byte aligned; it returns 0 for other lengths, for which ws may be NULL.  A missing
@@ -329,7 +329,8 @@ size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t Hq, int64_
  * behind m are left as they were; lens_out (device int32 [B], may be NULL) m.  dst->lens is not read and may be lens_out; lens_out must not be
  * src->lens, acc_out must not overlap acc, and the pages that dst names must not be among those of src (both may lie in one pool).
  * acc: device fp32, rows acc_stride >= max_len apart; NaN and infinity count as the largest finite number.  sink + recent <= budget (KVP_ERR_SHAPE);
- * dst->max_blocks * bs >= budget.  max_len as in kvp_cache_attend.  src and dst agree in B, H, bs and format. */
+ * dst->max_blocks * bs >= budget.  max_len as in kvp_cache_attend.  src and dst agree in B, H, bs and format.
+ * Limits: those of a cache; max_len < 2^30; B * H below 2^23, B * H * ceil(max_len / 1024) below 2^24. */
 int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64_t acc_stride, int64_t budget, int64_t sink, int64_t recent,
                         const kvp_cache* dst, int32_t* keep_idx, float* acc_out, int64_t acc_out_stride, int32_t* lens_out,
                         int64_t max_len, void* ws, size_t ws_bytes, void* stream);

@@ -279,7 +279,7 @@ extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64
     return KVP_ERR_ALIGN;
   if (lens_out == src->lens || acc_out == acc || dst->block_table == src->block_table) return KVP_ERR_SHAPE;
   const int64_t rows = src->B * src->H, pages = ceil_div(budget, src->bs), groups = ceil_div(max_len, 1024);
-  if (!fits_grid(rows * pages, kThreads) || !fits_grid(rows * groups, kThreads)) return KVP_ERR_SHAPE;
+  if (!fits_grid(rows * pages, kThreads) || !fits_grid(rows * groups, kThreads) || !select_fits(rows, max_len)) return KVP_ERR_SHAPE;
   const EvictLayout w = evict_layout(src->B, src->H, max_len, budget);
   if (!ws || ws_bytes < w.total || !aligned16(ws)) return KVP_ERR_WORKSPACE;
   EvictArgs a{};

@@ -759,6 +759,9 @@ SamplePlan make_sample_plan(int64_t T, int64_t k) {
 
 size_t select_workspace_bytes(int64_t n_rows, int64_t T) { return select_layout(n_rows, T).total; }
 
+// a block per row: 512 threads where a row is read once and there are many, otherwise 1024
+bool select_fits(int64_t n_rows, int64_t T) { return fits_grid(n_rows, T <= kSpan ? 512 : 1024); }
+
 void select_topk_launch(const float* scores, int64_t n_rows, int64_t T, int64_t row_stride, int64_t k,
                         int32_t* idx_out, void* ws, hipStream_t st) {
   const dim3 rows(static_cast<unsigned>(n_rows));
@@ -813,6 +816,7 @@ extern "C" int32_t kvp_select_topk(const float* scores, int64_t n_rows, int64_t 
     return KVP_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(scores) & 3u) || (reinterpret_cast<uintptr_t>(idx_out) & 3u)) return KVP_ERR_ALIGN;
   if (n_rows == 0 || k == 0) return KVP_OK;
+  if (!select_fits(n_rows, T)) return KVP_ERR_SHAPE;
   const size_t need = select_workspace_bytes(n_rows, T);
   if (need != 0 && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15u))) return KVP_ERR_WORKSPACE;
   select_topk_launch(scores, n_rows, T, row_stride, k, idx_out, ws, as_stream(stream));

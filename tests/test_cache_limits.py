@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 import paper_2512_14946_amd as kvp
-from test_cache_abi import SHAPE, WORKSPACE, attend, cache, view
+from test_cache_abi import SHAPE, WORKSPACE, attend, cache, evict, view
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -45,3 +45,18 @@ def _sized(B, H, G, W, T, **kw):
                                             (1 << 13, 8, 1, 130, 32768 - 128, WORKSPACE), (1 << 13, 8, 1, 130, 32768, SHAPE)])
 def test_shapes_on_either_side_of_the_limits(B, H, G, W, T, code):
     assert _sized(B, H, G, W, T) == code
+
+
+@pytest.mark.parametrize("B,H,code", [((1 << 23) - 1, 1, WORKSPACE), (1 << 21, 4, SHAPE)])
+def test_evict_refuses_more_rows_than_its_selection_takes(B, H, code):
+    # nothing may be enqueued: the pages would move by a list that no selection wrote
+    c = dict(B=B, H=H, max_blocks=1, table_stride=1, num_blocks=1)
+    assert evict(src=cache(**c), dst=cache(block_table=1 << 21, **c), budget=8, stride=16, ws=None) == code
+
+
+def test_selection_refuses_more_rows_than_a_grid_takes():
+    call = kvp.kvp._lib.kvp_select_topk
+    assert call(4096, 1 << 23, 16, 16, 4, 8192, None, 0, None) == SHAPE
+    need = kvp.kvp_select_workspace_bytes(1 << 22, 16400, 4)
+    assert call(4096, 1 << 22, 16400, 16400, 4, 8192, 4096, need, None) == SHAPE
+    assert call(4096, (1 << 22) - 1, 16400, 16400, 4, 8192, None, 0, None) == WORKSPACE

@@ -112,6 +112,13 @@ __device__ __forceinline__ void logits(const uint4 k[4][2], const half8_t qf[R][
   }
 }
 
+// What a lane has stored to LDS is there for the others of its wave: the compiler may not move accesses across, nor take the lanes apart.
+__device__ __forceinline__ void wave_step() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // LOGITS: they are kept for the weights (one row tile); SHARED: several row tiles; R: groups of 16 rows, which share every code's decoding
 template <int FMT, bool LOGITS, bool SHARED, int R>
 __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs a) {
@@ -272,11 +279,13 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
     if constexpr (MORE) load_values<SHARED>(a, cell_v, run + kStep, lane, v);
     if constexpr (LOGITS) {
       if (!MORE || n_kept == keep) {
+        wave_step();
         float4* to = reinterpret_cast<float4*>(a.logits + static_cast<int64_t>(cell) * a.M * a.logit_stride + static_cast<int64_t>(t - (n_kept - 1) * kTileTokens) * a.M);
         for (uint32_t i = lane; i < n_kept * a.M * 16; i += kWave) {
           const float4 u = reinterpret_cast<const float4*>(kept_s)[i];
           store_stream16(to + i, make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(u.z), __float_as_uint(u.w)));
         }
+        wave_step();   // read before the next tiles' overwrite it
         n_kept = 0;
       }
     }

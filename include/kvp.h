@@ -284,7 +284,7 @@ typedef struct {
  *     scale = max(scale before, fl32(a / qmax))       otherwise;
  *     where that raised the scale, the codes before become rnd(fl32(fl32(code * scale before) / scale)),
  *     new codes are rnd(fl32(x / scale)), 0 when scale is 0 (IEEE binary32 quotients, rounded half to even to whole
- *     numbers or to e4m3; the sign of a zero code is not specified).  Finite k and v: one that is not spoils its page.
+ *     numbers or to e4m3; the sign of a zero code is not specified; beyond +-qmax, which a subnormal scale allows, +-qmax).  Finite k and v: one that is not spoils its page.
  * Slots behind the last token keep their bytes.  Pages that get tokens must belong to one sequence only (pages shared
  * between sequences may be full ones).  Graph capture: nothing but kernels is enqueued. */
 int32_t kvp_cache_append(const kvp_cache* cache, const kvp_view* k, const kvp_view* v, const int32_t* counts, void* stream);

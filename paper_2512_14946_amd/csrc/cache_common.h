@@ -107,7 +107,8 @@ __device__ __forceinline__ half8_t decode8_half(uint32_t w0, uint32_t w1) {
 }
 
 // Codes of values on a given scale: rnd(fl32(x / scale)).  The quotient without a division per element, as in quant_device.h: the correctly
-// rounded reciprocal, a product and one remainder step.  Scales outside [2^-60, 2^60] divide.
+// rounded reciprocal, a product and one remainder step.  Scales outside [2^-60, 2^60] divide; a subnormal one may be off by up to a third (a
+// largest value of 1.49 qmax units of 2^-149 has a scale of one), and quotients beyond the largest code become that code.
 struct PageQuantizer {
   float scale, inv;
   bool unsafe;
@@ -126,6 +127,10 @@ struct PageQuantizer {
     float q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[i] = quotient(x[i]);
+    if (unsafe) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = fminf(fmaxf(q[i], -kCodeMax<FMT>), kCodeMax<FMT>);
+    }
     if constexpr (FMT == KVP_CACHE_INT8) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) q[i] = rintf(q[i]);

@@ -326,35 +326,35 @@ _CACHE_FORMATS = {"int8": KVP_CACHE_INT8, "e4m3": KVP_CACHE_E4M3}
 
 
 def _cache(c: KVCache) -> _Cache:
-    # like _paged: the marshalled struct is kept as long as it refers to the same tensors with the same metadata
-    k, v, ks, vs, t, n = c.k_codes, c.v_codes, c.k_scales, c.v_scales, c.block_table, c.lens
-    o = c.__dict__.get("_c")
-    if (o is not None and o[0] is k and o[1] is v and o[2] is ks and o[3] is vs and o[4] is t and o[5] is n and o[6] == c.fmt
-            and o[7] == k.data_ptr() and o[8] == v.data_ptr() and o[9] == ks.data_ptr() and o[10] == vs.data_ptr()
-            and o[11] == t.data_ptr() and o[12] == n.data_ptr() and o[13] == k.stride() and o[14] == v.stride() and o[15] == t.stride() and o[23] == ks.stride() and o[24] == vs.stride()
-            and o[16] == k.shape and o[17] == v.shape and o[18] == ks.shape and o[19] == vs.shape and o[20] == t.shape and o[21] == n.shape):
-        return o[22]
-    ts = (k, v, ks, vs, t, n)
+    # the marshalled struct is kept with everything that it is made of: tensors replaced or changed in place give a new one
+    k, v, ks, vs, t, n = ts = c.k_codes, c.v_codes, c.k_scales, c.v_scales, c.block_table, c.lens
+    key = (c.fmt, k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), t.data_ptr(), n.data_ptr(),
+           k.shape, v.shape, ks.shape, vs.shape, t.shape, n.shape,
+           k.stride(), v.stride(), ks.stride(), vs.stride(), t.stride(), n.stride(),
+           k.dtype, v.dtype, ks.dtype, vs.dtype, t.dtype, n.dtype)
+    kept = c.__dict__.get("_c")
+    if kept is not None and kept[0] == key:
+        return kept[1]
     if c.fmt not in _CACHE_FORMATS:
         raise ValueError('fmt must be "int8" or "e4m3"')
-    if c.k_codes.dtype != torch.uint8 or c.v_codes.dtype != torch.uint8 or c.k_codes.dim() != 4:
+    if k.dtype != torch.uint8 or v.dtype != torch.uint8 or k.dim() != 4:
         raise ValueError("codes must be uint8 [num_blocks][H][bs][D] and [num_blocks][H][D][bs]")
-    NB, H, bs, D = c.k_codes.shape
-    if tuple(c.v_codes.shape) != (NB, H, D, bs):
+    NB, H, bs, D = k.shape
+    if tuple(v.shape) != (NB, H, D, bs):
         raise ValueError("v_codes must be [num_blocks][H][D][bs]")
     for x in (ks, vs):
         if x.dtype != torch.float32 or tuple(x.shape) != (NB, H) or not x.is_contiguous():
             raise ValueError("scales must be contiguous float32 [num_blocks][H]")
-    if not (c.k_codes.is_contiguous() and c.v_codes.is_contiguous()):
+    if not (k.is_contiguous() and v.is_contiguous()):
         raise ValueError("codes must be contiguous")
     if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("block_table must be int32 [B][max_blocks] with contiguous rows")
-    if c.lens.dtype != torch.int32 or tuple(c.lens.shape) != (t.shape[0],) or not c.lens.is_contiguous():
+    if n.dtype != torch.int32 or tuple(n.shape) != (t.shape[0],) or not n.is_contiguous():
         raise ValueError("lens must be contiguous int32 [B]")
     _one_device(*ts)
     m = _Cache(*[x.data_ptr() for x in ts], t.shape[0], NB, bs, H, D, t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1],
                _CACHE_FORMATS[c.fmt])
-    c.__dict__["_c"] = (*ts, c.fmt, *[x.data_ptr() for x in ts], k.stride(), v.stride(), t.stride(), *[x.shape for x in ts], m, ks.stride(), vs.stride())
+    c.__dict__["_c"] = (key, m)
     return m
 
 

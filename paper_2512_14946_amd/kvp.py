@@ -380,7 +380,7 @@ def _weight_rows(t, B: int, H: int, n: int, what: str):
     """(pointer, row stride) of float32 [B][H][>= n] whose B * H rows are equally far apart."""
     if t.dtype != torch.float32 or t.dim() != 3 or tuple(t.shape[:2]) != (B, H) or t.shape[2] < n or (t.shape[2] > 1 and t.stride(2) != 1):
         raise ValueError(f"{what} must be float32 [B][H][n] with contiguous rows of at least {n} entries")
-    stride = t.stride(1) if H > 1 else t.stride(0) if B > 1 else t.shape[2]
+    stride = t.stride(1) if H > 1 else t.stride(0) if B > 1 else n      # one row: no distance
     if B > 1 and H > 1 and t.stride(0) != H * t.stride(1):
         raise ValueError(f"the rows of {what} must be equally far apart")
     return t.data_ptr(), stride

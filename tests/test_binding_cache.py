@@ -19,3 +19,10 @@ def test_cache_struct_follows_tensors_changed_in_place(monkeypatch):
     c.k_scales.data = c.k_scales.view(torch.int32)
     with pytest.raises(ValueError, match="scales"):
         binding._cache(c)
+
+
+def test_the_distance_of_a_single_row_does_not_matter():
+    a, b = torch.zeros(1, 1, 100), torch.zeros(1, 3, 200)[:, 1:2]
+    assert binding._weight_rows(a, 1, 1, 90, "acc_in")[1] == binding._weight_rows(b, 1, 1, 90, "acc_out")[1] == 90
+    assert binding._weight_rows(torch.zeros(2, 1, 100), 2, 1, 90, "acc")[1] == 100
+    assert binding._weight_rows(torch.zeros(1, 2, 100)[..., 5:], 1, 2, 90, "acc")[1] == 100

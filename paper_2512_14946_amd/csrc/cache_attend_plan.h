@@ -58,7 +58,9 @@ inline AttendPlan make_attend_plan_of(int64_t tile_rows, int64_t B, int64_t H, i
   // 34, 40 (4 x 4 x 30000), 89, 90 (4 x 4 x 131072, 7 rows), 49, 62 (8 x 2048, 2048 rows); 480 against 192: 76, 87 (4 x 4 x 30000, 96 rows).
   // More than a round only for chunks that outweigh their partial results: 1056 blocks in 5 rounds against 264 in 2: 146, 200 (33 x 8 x 12000, 4
   // rows); but 45, 38 with chunks of 768 (130 x 2 x 2100), and 84, 78 with 2000 for 528 cells (33 x 8 x 4000, 28 rows).
-  // (Times of tiles of 16 and 256.)
+  // Those are times of tiles of 16 and 256.  Tiles of 32, us with 1, 2, 3, 4, 5, 8 chunks, and with what the rule takes: 73, 89, 95, 101, 109, 124, 73 (16 x 8 x
+  // 8192 keys, 64 rows); 190, 104, 76, 60, 53, 66, 53 (4 x 4 x 30000, 96); 212, 191, 183, 189, 184, 207, 189 (33 x 8 x 12000, 20); 71, 48, 63, 54, 51, 57, 51
+  // (12 x 8 x 8192, 20); 131, 78, 98, 82, 74, 77, 73 (3 x 8 x 20000, 128); 203, 110, 78, 61, 52, 37, 33 (1 x 8 x 32768, 96).
   const int64_t first = std::max<int64_t>(1, kUnits / p.cells);
   const int64_t last = std::min(first + 8, std::max(first, T / (p.tile_rows == kManyRows ? 4096 : p.cells < kUnits ? 1024 : 2048)));
   int64_t n = first;

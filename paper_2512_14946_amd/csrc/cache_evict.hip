@@ -120,7 +120,10 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(const EvictArgs a)
   __syncthreads();   // the stretches
 
   // Values lie channel by channel, so a token touches every 64 bytes of its page: pages are read whole, the next while this one's tokens
-  // are picked.  Few tokens per page (a quarter or less of what would fill it on the whole): byte by byte, all at once.
+  // are picked.  More than four pages that average fewer than four tokens each: byte by byte, all at once.  Whole call and a read, us,
+  // always by bytes, always by pages (8 x 8 x 16384, kept 8192, 4096, 2048, 1024, 512, 200):
+  //   64-token pages   217 167, 124 109, 79 85, 63 67, 51 73, 35 85;    this rule 161, 106, 83, 69, 51, 39
+  //   16-token pages   254 214, 140 128, 83 85, 53 58, 35 39, 28 34;    this rule 208, 138, 87, 54, 36, 28
   float amax = 0.0f;
   const bool bytes = stretches * 4 > live && stretches > 4;
   uint4 page[(ITEMS + 1) / 2];

@@ -328,12 +328,13 @@ size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t Hq, int64_
  * indices, -1 behind m; acc_out (device fp32, rows acc_out_stride >= budget apart, may be NULL) the kept weights, entries
  * behind m are left as they were; lens_out (device int32 [B], may be NULL) m.  dst->lens is not read and may be lens_out; lens_out must not be
  * src->lens, acc_out must not overlap acc, and the pages that dst names must not be among those of src (both may lie in one pool).
- * acc: device fp32, rows acc_stride >= max_len apart; NaN and infinity count as the largest finite number.  sink + recent <= budget (KVP_ERR_SHAPE);
+ * acc: device fp32, rows acc_stride >= max_len apart; NaN and +infinity count as the largest finite number.  sink + recent <= budget (KVP_ERR_SHAPE);
  * dst->max_blocks * bs >= budget.  max_len as in kvp_cache_attend.  src and dst agree in B, H, bs and format.
  * Limits: those of a cache; max_len < 2^30; B * H below 2^23, B * H * ceil(max_len / 1024) below 2^24. */
 int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64_t acc_stride, int64_t budget, int64_t sink, int64_t recent,
                         const kvp_cache* dst, int32_t* keep_idx, float* acc_out, int64_t acc_out_stride, int32_t* lens_out,
                         int64_t max_len, void* ws, size_t ws_bytes, void* stream);
+/* T: max_len.  A workspace for some T serves every smaller one. */
 size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t T, int64_t budget);
 
 /* Rotary positions of queries or keys: the pairs of the first rotary_dim channels of every row of x turn by

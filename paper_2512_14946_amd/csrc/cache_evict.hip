@@ -260,7 +260,8 @@ extern "C" size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t 
   constexpr int64_t kMost = 1ll << 31;   // what a call accepts: nothing below overflows
   if (B <= 0 || H <= 0 || T <= 0 || budget <= 0) return 0;
   if (B >= kMost || H >= kMost || B * H >= kMost || T >= (1ll << 30) || budget >= kMost) return 0;
-  return kvp::evict_layout(B, H, T, budget).total;
+  // scratch that serves every smaller T: the selection's too, which rows beyond kMaxSplitT do without
+  return std::max(kvp::evict_layout(B, H, T, budget).total, kvp::evict_layout(B, H, std::min(T, kvp::kMaxSplitT), budget).total);
 }
 
 extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64_t acc_stride, int64_t budget, int64_t sink,

@@ -11,6 +11,7 @@ int32_t score_tokens_impl(const kvp_view* q_win, const kvp_view* k, int32_t caus
 
 // kvp_select_topk's kernel launches; arguments already validated, n_rows > 0, 0 < k <= T, select_fits(n_rows, T); ws holds at least
 // select_workspace_bytes(n_rows, T) bytes, 16-byte aligned (may be null when that is 0).
+constexpr int64_t kMaxSplitT = 1 << 18;        // rows up to this length may need scratch, longer ones need none
 size_t select_workspace_bytes(int64_t n_rows, int64_t T);
 bool select_fits(int64_t n_rows, int64_t T);   // the rows' blocks fit a grid
 void select_topk_launch(const float* scores, int64_t n_rows, int64_t T, int64_t row_stride, int64_t k,

@@ -44,7 +44,6 @@ constexpr int kCopies = 4;            // interleaved histogram copies (lane & 3)
 constexpr int kRowCap = 16384;        // candidates per row (what a 1024-thread block holds in registers)
 constexpr int kLaneCap = 8;           // candidates one thread can stage per span
 constexpr int kFineShift = 18;        // sample histogram: 32 bins per octave, 64 octaves below the maximum
-constexpr int64_t kMaxSplitT = 1 << 18;
 
 // Block shapes: THREADS threads hold a span as ITEMS float4 items each.
 template <int THREADS>

@@ -60,3 +60,13 @@ def test_selection_refuses_more_rows_than_a_grid_takes():
     need = kvp.kvp_select_workspace_bytes(1 << 22, 16400, 4)
     assert call(4096, 1 << 22, 16400, 16400, 4, 8192, 4096, need, None) == SHAPE
     assert call(4096, (1 << 22) - 1, 16400, 16400, 4, 8192, None, 0, None) == WORKSPACE
+
+
+@pytest.mark.parametrize("rows,budget", [(1, 16), (3, 100000), (64, 4096)])
+def test_an_eviction_workspace_serves_every_smaller_bound(rows, budget):
+    # rows of 2^14 + 1 to 2^18 weights need scratch for their selection, longer ones none
+    before = 0
+    for T in [1, 100, 16384, 16385, 20000, 250000, (1 << 18) - 1, 1 << 18, (1 << 18) + 1, 270000, 278000, 290000, 1 << 20]:
+        need = kvp.kvp_cache_evict_workspace_bytes(rows, 1, T, budget)
+        assert need >= before, T
+        before = need

@@ -455,7 +455,8 @@ extern "C" size_t kvp_cache_attend_workspace_bytes(int64_t B, int64_t H, int64_t
   constexpr int64_t kMost = 1ll << 31, kRows = 1ll << 24;   // what a call accepts: nothing below overflows
   if (B <= 0 || H <= 0 || Hq <= 0 || Hq % H || W <= 0 || T <= 0) return 0;
   if (B >= kMost || H >= kMost || B * H >= kMost || T >= kMost || W >= kRows || Hq / H >= kRows || Hq / H * W >= kRows) return 0;
-  return kvp::make_attend_plan(B, H, Hq, W, T, weights != 0).bytes;
+  const kvp::AttendPlan p = kvp::make_attend_plan(B, H, Hq, W, T, weights != 0);
+  return kvp::attend_fits(kvp::attend_blocks(p, B * H, Hq / H * W, T, weights != 0)) ? p.bytes : 0;
 }
 
 extern "C" int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,

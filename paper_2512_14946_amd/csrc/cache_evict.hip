@@ -16,6 +16,7 @@ namespace kvp {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kRankTokens = 4 * kThreads;   // tokens of a block that ranks
 
 struct EvictArgs {
   CacheArgs src, dst;
@@ -33,7 +34,7 @@ struct EvictArgs {
 __device__ __forceinline__ uint32_t evict_len(const EvictArgs& a, uint32_t b) { return min(cache_len(a.src, b), a.T); }
 
 __global__ __launch_bounds__(kThreads) void evict_rank_kernel(const EvictArgs a, uint32_t groups, FastDiv div_groups) {
-  const uint32_t bh = div_groups.quot(blockIdx.x), t0 = (blockIdx.x - bh * groups) * 1024 + threadIdx.x;
+  const uint32_t bh = div_groups.quot(blockIdx.x), t0 = (blockIdx.x - bh * groups) * kRankTokens + threadIdx.x;
   const uint32_t n = evict_len(a, a.div_h.quot(bh));
   const float* acc = a.acc + static_cast<int64_t>(bh) * a.acc_stride;
   float* rank = a.rank + static_cast<int64_t>(bh) * a.T;
@@ -238,6 +239,9 @@ void move_launch(const EvictArgs& a, dim3 grid, hipStream_t st) {
   }
 }
 
+// the launches that rank and select fit a grid
+bool rows_fit(int64_t rows, int64_t T) { return fits_grid(rows * ceil_div(T, kRankTokens), kThreads) && select_fits(rows, T); }
+
 struct EvictLayout {
   size_t rank, kept, select, total;
 };
@@ -260,6 +264,7 @@ extern "C" size_t kvp_cache_evict_workspace_bytes(int64_t B, int64_t H, int64_t 
   constexpr int64_t kMost = 1ll << 31;   // what a call accepts: nothing below overflows
   if (B <= 0 || H <= 0 || T <= 0 || budget <= 0) return 0;
   if (B >= kMost || H >= kMost || B * H >= kMost || T >= (1ll << 30) || budget >= kMost) return 0;
+  if (!kvp::rows_fit(B * H, T)) return 0;
   // scratch that serves every smaller T: the selection's too, which rows beyond kMaxSplitT do without
   return std::max(kvp::evict_layout(B, H, T, budget).total, kvp::evict_layout(B, H, std::min(T, kvp::kMaxSplitT), budget).total);
 }
@@ -282,8 +287,8 @@ extern "C" int32_t kvp_cache_evict(const kvp_cache* src, const float* acc, int64
        reinterpret_cast<uintptr_t>(lens_out)) & 3u)
     return KVP_ERR_ALIGN;
   if (lens_out == src->lens || acc_out == acc || dst->block_table == src->block_table) return KVP_ERR_SHAPE;
-  const int64_t rows = src->B * src->H, pages = ceil_div(budget, src->bs), groups = ceil_div(max_len, 1024);
-  if (!fits_grid(rows * pages, kThreads) || !fits_grid(rows * groups, kThreads) || !select_fits(rows, max_len)) return KVP_ERR_SHAPE;
+  const int64_t rows = src->B * src->H, pages = ceil_div(budget, src->bs), groups = ceil_div(max_len, kRankTokens);
+  if (!fits_grid(rows * pages, kThreads) || !rows_fit(rows, max_len)) return KVP_ERR_SHAPE;
   const EvictLayout w = evict_layout(src->B, src->H, max_len, budget);
   if (!ws || ws_bytes < w.total || !aligned16(ws)) return KVP_ERR_WORKSPACE;
   EvictArgs a{};

@@ -70,3 +70,11 @@ def test_an_eviction_workspace_serves_every_smaller_bound(rows, budget):
         need = kvp.kvp_cache_evict_workspace_bytes(rows, 1, T, budget)
         assert need >= before, T
         before = need
+
+
+def test_sizes_behind_the_limits_have_no_workspace():
+    m = (1 << 31) - 1
+    assert kvp.kvp_cache_attend_workspace_bytes(m, 1, 1, 1, m, True) == 0            # logits of 2^62 tokens: a product that wraps
+    assert kvp.kvp_cache_attend_workspace_bytes(1 << 19, 16, 16, 16, 16, True) == 0 < kvp.kvp_cache_attend_workspace_bytes(1 << 19, 15, 15, 16, 16, True)
+    assert kvp.kvp_cache_evict_workspace_bytes(1 << 21, 4, 16, 8) == 0 < kvp.kvp_cache_evict_workspace_bytes(1 << 21, 3, 16, 8)
+    assert kvp.kvp_cache_evict_workspace_bytes(1 << 13, 1 << 9, 1 << 20, 8) == 0

@@ -309,9 +309,9 @@ int32_t kvp_cache_read(const kvp_cache* cache, const int32_t* first, const kvp_v
  * Arithmetic: queries are split exactly into a power of two per row and 16-bit values (what lies 2^-24 below the row's
  * largest element is rounded away), codes are exact in 16 bits, the products of both contractions run on the matrix cores
  * with fp32 accumulation, logits, statistics and sums are fp32; for the product with V a probability times its page's value
- * scale is rounded to 11 bits (2^-11 relative) or to 2^-35 of the row's largest probability times the largest value scale,
- * 2^-100 at least, whichever is coarser.  Finite q and cache contents, finite scale: a row that does not see a token is still
- * spoiled by a value of it that is not finite.
+ * scale is rounded to 11 bits (2^-11 relative), for W * G up to 16 to 22 bits, or to 2^-35 of the row's largest probability
+ * times the largest value scale, 2^-100 at least, whichever is coarser.  Finite q and cache contents, finite scale: a row that
+ * does not see a token is still spoiled by a value of it that is not finite.
  * Limits: those of a cache; W * G below 2^24; B * H * ceil(W * G / 256), for W * G up to 128 B * H * ceil(W * G / 16), below 2^23 - 7;
  * with acc_out B * H * ceil(max_len / 128) below 2^24. */
 int32_t kvp_cache_attend(const kvp_view* q, const kvp_cache* cache, const int32_t* q_lens, int32_t causal, float scale,

@@ -11,6 +11,10 @@
 // halves hold them).  Logits are kept in base 2.  The reference that exponentials are taken against is set 2^10 below the maximum and follows it
 // lazily: it moves only when a probability times its page's share exceeds 2^15.5, which halves and the sums in fp32 bear.
 //
+// A probability has 11 bits as a half, while the result is rounded to the 8 of bf16.  Where a call has one tile of 16 rows it is taken as two halves, 22 bits,
+// which costs nothing beside the memory (us with one, two: 89.3, 89.5 for 4 x 4 x 131072 tokens, 7 rows; 154.6, 155.0 for 33 x 8 x 12000, 4 rows; 12.3 both
+// for 8 x 4096).  More rows keep one: 53.9, 55.3 (16 x 8 x 8192, 20 rows), 71.6, 82.2 (64 rows), 1001, 1363 (4 x 8 x 16384, 4096 rows).
+//
 // This file: up to 128 query rows per (sequence, head) in tiles of 16 or 32, a decode step above all, bound by HBM.  A block's waves take a quarter
 // of its chunk each, with the loads of the next 64 tokens always in flight; partial results of chunks are joined by a second kernel.
 // The weights of the tokens need the final statistics of their rows: up to 16 rows the logits are kept and the second kernel sums them.
@@ -123,6 +127,7 @@ __device__ __forceinline__ void wave_step() {
 template <int FMT, bool LOGITS, bool SHARED, int R>
 __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs a) {
   constexpr int kRows = 16 * R, kOutFloats = kRows * kOutPitch;
+  constexpr int kParts = SHARED || R > 1 ? 1 : 2;   // halves of a probability
   __shared__ __attribute__((aligned(16))) float shared_s[kWaves * (LOGITS ? kKeptFloats : kOutFloats)];   // kept logits, then the waves' results
   __shared__ float ref_s[kWaves][kRows], sum_s[kWaves][kRows], val_s[kWaves];
   uint32_t cell, chunk;
@@ -254,7 +259,7 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       log_share = fmaxf(__builtin_amdgcn_logf(vs_now * inv_vref), -60.0f);
     }
     const float per_share = __builtin_amdgcn_exp2f(-log_share);
-    half8_t pf[R][2];
+    half8_t pf[kParts][R][2];
 #pragma unroll
     for (int u = 0; u < R; ++u) {
       const float off = log_share - ref[u];
@@ -266,7 +271,11 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       }
       sum[u] = fmaf(part, per_share, sum[u]);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) pf[u][i >> 3][i & 7] = static_cast<_Float16>(p[i]);
+      for (int i = 0; i < 16; ++i) {
+        const _Float16 x = static_cast<_Float16>(p[i]);
+        pf[0][u][i >> 3][i & 7] = x;
+        if constexpr (kParts > 1) pf[1][u][i >> 3][i & 7] = static_cast<_Float16>(p[i] - static_cast<float>(x));
+      }
     }
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -274,7 +283,9 @@ __global__ __launch_bounds__(kThreads) void cache_attend_kernel(const AttendArgs
       for (int c = 0; c < 8; ++c) {
         const half8_t x = half ? decode8_half<FMT>(v[c].z, v[c].w) : decode8_half<FMT>(v[c].x, v[c].y);
 #pragma unroll
-        for (int u = 0; u < R; ++u) o[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pf[u][half], o[u][c], 0, 0, 0);
+        for (int u = 0; u < R; ++u)
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) o[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pf[part][u][half], o[u][c], 0, 0, 0);
       }
     if constexpr (MORE) load_values<SHARED>(a, cell_v, run + kStep, lane, v);
     if constexpr (LOGITS) {

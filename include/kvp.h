@@ -187,8 +187,8 @@ size_t kvp_score_keys_workspace_bytes(int64_t L, int64_t H, int64_t T, int32_t m
  * of n_rows rows of T fp32 scores (row_stride floats apart): the indices of the
  * k largest, equal scores resolved toward the lowest index, written ascending
  * to idx_out [n_rows][k] (device int32).  NaN scores are out of contract.
- * 0 <= k <= T; T < 2^30; fewer than 2^23 rows, 2^22 of more than 16384 scores.  Rows longer than 16384 and up to 2^18 scores are split over several
- * workgroups and need scratch: kvp_select_workspace_bytes(n_rows, T, k) bytes (16 bytes for two
+ * 0 <= k <= T; T < 2^30; fewer than 2^23 rows, or 2^22 of more than 16384 scores (KVP_ERR_SHAPE).
+ * Rows longer than 16384 and up to 2^18 scores are split over several workgroups and need scratch: kvp_select_workspace_bytes(n_rows, T, k) bytes (16 bytes for two
  * pivots and a flag per row, two counts per 16384-score span, 64 KiB of candidate slots per
  * row), 16-byte aligned; it returns 0 for other lengths, for which ws may be NULL.  A missing
  * or short workspace: KVP_ERR_WORKSPACE. */
@@ -284,7 +284,8 @@ typedef struct {
  *     scale = max(scale before, fl32(a / qmax))       otherwise;
  *     where that raised the scale, the codes before become rnd(fl32(fl32(code * scale before) / scale)),
  *     new codes are rnd(fl32(x / scale)), 0 when scale is 0 (IEEE binary32 quotients, rounded half to even to whole
- *     numbers or to e4m3; the sign of a zero code is not specified; beyond +-qmax, which a subnormal scale allows, +-qmax).  Finite k and v: one that is not spoils its page.
+ *     numbers or to e4m3; the sign of a zero code is not specified; beyond +-qmax, which a subnormal scale allows, +-qmax).
+ * Finite k and v: one that is not spoils its page.
  * Slots behind the last token keep their bytes.  Pages that get tokens must belong to one sequence only (pages shared
  * between sequences may be full ones).  Graph capture: nothing but kernels is enqueued. */
 int32_t kvp_cache_append(const kvp_cache* cache, const kvp_view* k, const kvp_view* v, const int32_t* counts, void* stream);

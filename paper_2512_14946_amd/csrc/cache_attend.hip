@@ -12,14 +12,14 @@
 // lazily: it moves only when a probability times its page's share exceeds 2^15.5, which halves and the sums in fp32 bear.
 //
 // A probability has 11 bits as a half, while the result is rounded to the 8 of bf16.  Where a call has one tile of 16 rows it is taken as two halves, 22 bits,
-// which costs nothing beside the memory (us with one, two: 89.3, 89.5 for 4 x 4 x 131072 tokens, 7 rows; 154.6, 155.0 for 33 x 8 x 12000, 4 rows; 12.3 both
-// for 8 x 4096).  More rows keep one: 53.9, 55.3 (16 x 8 x 8192, 20 rows), 71.6, 82.2 (64 rows), 1001, 1363 (4 x 8 x 16384, 4096 rows).
+// which costs half a percent beside the memory (us with one, two: 89.0, 89.3 for 4 x 4 x 131072 tokens, 7 rows; 154.6, 155.0 for 33 x 8 x 12000, 4 rows;
+// 11.3 both for 8 x 4096).  More rows keep one: 53.9, 55.3 (16 x 8 x 8192, 20 rows), 71.6, 82.2 (64 rows), 1001, 1363 (4 x 8 x 16384, 4096 rows).
 //
 // This file: up to 128 query rows per (sequence, head) in tiles of 16 or 32, a decode step above all, bound by HBM.  A block's waves take a quarter
 // of its chunk each, with the loads of the next 64 tokens always in flight; partial results of chunks are joined by a second kernel.
 // The weights of the tokens need the final statistics of their rows: up to 16 rows the logits are kept and the second kernel sums them.
 // More rows, and the weights of more than 16: cache_attend_rows.hip.
-// 4 x 4 x 131072 tokens, 7 rows: 89 us, 6.06 TB/s (a copy reaches 6.5); 64 x 8 x 16384 (ragged, three quarters of that), 8 rows: 281 us, 5.7 TB/s,
+// 4 x 4 x 131072 tokens, 7 rows: 89 us, 6.06 TB/s (a copy reaches 6.5); 64 x 8 x 16384 (ragged, three quarters of that), 8 rows: 285 us, 5.6 TB/s,
 // and 435 with weights: the logits cost 12 us to keep, 78 to store beside the reads, and the joining kernel takes 54; 8 x 4096, 4 rows: 11 us,
 // two launches and the latency of length, table, scale and code.  Decoding holds several tiles: 16 x 8 x 8192 tokens take 54 us for 20 rows
 // and 118 for 96.

@@ -6,7 +6,7 @@
 // and 32 of the 64 tokens, which are those that its operand of O^T = V^T P^T takes if the values' tokens are dealt out in the same order, so
 // probabilities stay in the lane.  A tile has four runs of 16 tokens; a run lies in one page, so scales are uniform over the wave.
 // The halves of a block are half a tile apart, so that one's products run beside the other's exponentials.  4 x 8 x 16384 keys, 4096 rows
-// (causal): 1.00 to 1.08 ms on two cards, 1.06 to 0.99 PFLOP/s; a large library product of halves reaches 1.20.  Bound by power: 3500
+// (causal): 1.00 to 1.09 ms, by the card, 1.06 to 0.97 PFLOP/s; a large library product of halves reaches 1.20.  Bound by power: 3500
 // cycles a tile where the products alone take 2048 and the exponentials and staging 2300, at 1.75 GHz of 2.4.
 // A probability is one half, of 11 bits for a result of 8: two, as for few rows, take 1.36 ms, and 387 us for 322 of 2 x 4 ragged to 30011 keys, 1421 rows.
 // Measured against it at the same sizes, ms: both halves in step 1.03; 64 rows per wave, four waves 1.43 to 1.79; two blocks of 128 rows per CU
